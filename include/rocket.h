@@ -347,6 +347,108 @@ int rocket_train_step(rocket_kernels *kernels, const void *x_dev, int x_is_u8, i
                       void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Layer norm of the pooled features.  The planes of a feature row live on different scales (maxima around 8, shares in
+ * [0, 1]), so a plane of an example is a row of its own: for each of rows * planes rows of n values
+ *     m = mean x,  v = mean (x - m)^2,  r = 1 / sqrt(v + eps),  y = (x - m) r weight + bias
+ * with the weights and biases of its plane.  planes = 1 is the ordinary layer norm over n values.
+ *
+ * rocket_layer_norm: x_dev and y_dev (device, rows x planes x n of type dtype: ROCKET_F32, ROCKET_BF16 or ROCKET_F16; y_dev
+ * may be x_dev), weight_dev and bias_dev (device, planes x n float32, either may be NULL: 1 and 0), mean_dev and rstd_dev
+ * (device, rows x planes float32, both or neither NULL) receive m and r for the backward pass.  rows, planes, n >= 1,
+ * eps > 0.
+ *
+ * rocket_layer_norm_backward: from grad_y_dev (type dtype) and the forward pass's x, mean and rstd, with g = grad_y weight
+ * and h = (x - m) r
+ *     grad_x = r (g - mean g - h mean(g h)),   grad_weight = sum over rows of grad_y h,   grad_bias = sum of grad_y
+ * grad_x_dev (type dtype) may be grad_y_dev; grad_weight_dev and grad_bias_dev (device, planes x n float32) may be NULL.
+ * The rounding of mean_dev to 32 bits is made good from the row itself, so rows whose mean is large against their spread
+ * lose nothing by it.  The given rstd_dev is used as it stands.
+ *
+ * Statistics and sums are fp32 or wider and taken in a fixed order without atomics: the same call gives the same bits
+ * (not the same as another number of rows would, for the sums over rows).  A row that holds a NaN or an infinity becomes NaN
+ * as the formulas have it and leaves the other rows as they are (grad_weight and grad_bias sum over it).
+ * workspace_dev: rocket_layer_norm_workspace_bytes(rows, planes, n, backward) bytes of device memory, 256-byte aligned;
+ * the forward pass needs none (0 bytes, NULL allowed) unless rows are longer than a workgroup holds.  0 on invalid sizes.
+ * Every pointer is of the device that is current and of elements of its type (any element's address will do).
+ * Asynchronous on hip_stream, allocates nothing, may be captured.
+ */
+enum { ROCKET_F32 = 0, ROCKET_BF16 = 1, ROCKET_F16 = 2 };
+size_t rocket_layer_norm_workspace_bytes(int32_t rows, int32_t planes, int32_t n, int backward);
+int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows, int32_t planes, int32_t n, const float *weight_dev,
+                      const float *bias_dev, float eps, void *y_dev, float *mean_dev, float *rstd_dev,
+                      void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_dev, int32_t dtype, int32_t rows, int32_t planes,
+                               int32_t n, const float *weight_dev, const float *mean_dev, const float *rstd_dev,
+                               void *grad_x_dev, float *grad_weight_dev, float *grad_bias_dev,
+                               void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Many tensors at once: the global norm of all gradients, clipping, and an update that clips on the way.
+ * A list is a host array of `tensors` records; data is device memory (any element's address), count may be 0 (data is then
+ * not looked at).  Lists are read during the call only.
+ *
+ * rocket_grad_norm: norm = sqrt(sum of the squares of all values of all tensors), and the coefficient that brings a larger
+ * norm down to max_norm: norm_dev[0] = norm, norm_dev[1] = norm <= max_norm ? 1 : max_norm / norm (device, 2 doubles).
+ * max_norm > 0 (INFINITY: never clips).  Squares and sums are fp64, so no finite gradient overflows or vanishes, in a fixed
+ * order without atomics.  A NaN among the values makes both NaN; an infinity makes the norm infinite and the coefficient 0.
+ *
+ * rocket_grad_clip: rocket_grad_norm, then out[i] = grads[i] * coefficient, rounded once.  out: a list of the same counts and
+ * types (each its own gradient tensor, or overlapping none), or NULL: in place; where the coefficient is 1 nothing is then
+ * written.
+ *
+ * rocket_sgd_tensors: out[i] = params[i] - lr * coefficient * grads[i], in fp64, rounded once; params and out are
+ * ROCKET_F32, grads of any type, counts equal, out NULL: in place.  coefficient = norm_dev[1], or 1 where norm_dev is NULL.
+ * No pass over the gradients but this one: the clipped gradients are never stored.
+ *
+ * rocket_sgd_update_clipped: rocket_sgd_update with lr * coefficient in place of lr.
+ *
+ * workspace_dev: rocket_grad_workspace_bytes(grads, tensors) bytes, 256-byte aligned (0 for invalid lists).  Asynchronous on
+ * hip_stream, allocates nothing, may be captured (the recorded calls keep the addresses of the list).
+ */
+typedef struct rocket_tensor {
+    void *data;
+    int64_t count;
+    int32_t dtype;      /* ROCKET_F32, ROCKET_BF16, ROCKET_F16 */
+    int32_t reserved;   /* 0 */
+} rocket_tensor;
+size_t rocket_grad_workspace_bytes(const rocket_tensor *grads, int32_t tensors);
+int rocket_grad_norm(const rocket_tensor *grads, int32_t tensors, double max_norm, double *norm_dev,
+                     void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor *out, int32_t tensors, double max_norm,
+                     double *norm_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+int rocket_sgd_tensors(const rocket_tensor *params, const rocket_tensor *grads, const rocket_tensor *out, int32_t tensors,
+                       double lr, const double *norm_dev, void *hip_stream);
+int rocket_sgd_update_clipped(rocket_kernels *kernels, const float *grad_w_dev, const float *grad_b_dev, float lr,
+                              int recentre, const double *norm_dev, void *hip_stream);
+
+/*
+ * Inference and training with a layer norm between the features and the linear head: each feature plane of an example is
+ * normalised (planes = rocket_num_features(mask), n = K), norm_weight_dev and norm_bias_dev (device, F*K float32) belong to
+ * the model beside the kernels.
+ *
+ * rocket_infer_normed: rocket_infer with the head applied to the normalised features; features_dev receives those.
+ * norm_weight_dev and norm_bias_dev may be NULL.  workspace_dev: rocket_infer_normed_workspace_bytes(kernels, B, mask).
+ *
+ * rocket_train_step_normed: one step on the kernels' weights and biases and on norm_weight and norm_bias: transform, layer
+ * norm, prediction, loss gradient, both backward passes, the global norm over all four gradients, and the updates by
+ * lr * min(1, max_norm / norm).  *loss_dev (may be NULL) receives the loss before the update, norm_dev (2 doubles, may be
+ * NULL) norm and coefficient.  The other arguments are those of rocket_train_step.  B <= 65535.  A call that is refused leaves
+ * all parameters as they were.
+ * workspace_dev: rocket_train_normed_workspace_bytes(kernels, B, mask) bytes, 256-byte aligned.
+ */
+size_t rocket_infer_normed_workspace_bytes(const rocket_kernels *kernels, int32_t B, uint32_t feature_mask);
+int rocket_infer_normed(rocket_kernels *kernels, const void *x_dev, int x_is_u8, int32_t B, uint32_t feature_mask,
+                        float lambda, float shift, const float *norm_weight_dev, const float *norm_bias_dev, float eps,
+                        const double *coef_dev, const double *intercept_dev, float *features_dev, double *pred_dev,
+                        void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+size_t rocket_train_normed_workspace_bytes(const rocket_kernels *kernels, int32_t B, uint32_t feature_mask);
+int rocket_train_step_normed(rocket_kernels *kernels, const void *x_dev, int x_is_u8, int32_t B, uint32_t feature_mask,
+                             float lambda, float shift, float *norm_weight_dev, float *norm_bias_dev, float eps,
+                             const double *coef_dev, const double *intercept_dev, const float *targets_dev, float lr,
+                             int recentre, double max_norm, double *loss_dev, double *norm_dev,
+                             void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
  * MINIROCKET-style variant.  The paper describes MINIROCKET in its related-work section only (section 2) and
  * names it as the extension to build next (section 6): two-valued kernels, so that the convolution needs
  * additions only; weights from a predetermined set; biases sampled from the input data; PPV as the only

@@ -18,12 +18,12 @@ DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-pa
 
 KERNEL_TUS = ("rocket_forward.hip", "rocket_forward_soft.hip", "rocket_forward_short.hip", "rocket_forward_short_soft.hip", "rocket_forward_series.hip", "rocket_forward_groups.hip", "rocket_backward.hip", "rocket_backward_short.hip", "rocket_backward_groups.hip", "rocket_ridge.hip",
               "rocket_prologue.hip", "rocket_train.hip", "rocket_calibrate.hip", "rocket_minirocket.hip",
-              "rocket_minirocket_forward.hip")   # translation units that hold device code
-HOST_TUS = ("rocket_api.hip",)
+              "rocket_minirocket_forward.hip", "rocket_layer_norm.hip", "rocket_tensors.hip")   # translation units that hold device code
+HOST_TUS = ("rocket_api.hip", "rocket_normed.hip")
 
 
 def sources():
-    names = ("sampler.cpp", "rocket_internal.hpp", "rocket_device.hpp", "rocket_forward_impl.hpp", "rocket_backward_impl.hpp", "rocket_limbs.hpp") + KERNEL_TUS + HOST_TUS
+    names = ("sampler.cpp", "rocket_internal.hpp", "rocket_device.hpp", "rocket_forward_impl.hpp", "rocket_backward_impl.hpp", "rocket_limbs.hpp", "rocket_elements.hpp") + KERNEL_TUS + HOST_TUS
     return [os.path.join(CSRC, f) for f in names] + [os.path.join(ROOT, "include", "rocket.h")]
 
 

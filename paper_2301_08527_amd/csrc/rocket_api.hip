@@ -953,11 +953,12 @@ extern "C" int rocket_mse_grad(const double *pred_dev, const float *targets_dev,
     return ROCKET_OK;
 }
 
-extern "C" int rocket_sgd_update(rocket_kernels *h, const float *grad_w_dev, const float *grad_b_dev, float lr,
-                                 int recentre, void *hip_stream)
+// the update without (norm_dev null) and with the coefficient that clips the gradients
+static int sgd_update_impl(const char *fn, rocket_kernels *h, const float *grad_w_dev, const float *grad_b_dev, float lr,
+                           int recentre, const double *norm_dev, void *hip_stream)
 {
-    if (!h || !grad_w_dev || !grad_b_dev) return rk_fail(ROCKET_EINVAL, "rocket_sgd_update: NULL argument");
-    if (!std::isfinite(lr)) return rk_fail(ROCKET_EINVAL, "rocket_sgd_update: lr must be finite");
+    if (!h || !grad_w_dev || !grad_b_dev) return rk_fail(ROCKET_EINVAL, std::string(fn) + ": NULL argument");
+    if (!std::isfinite(lr)) return rk_fail(ROCKET_EINVAL, std::string(fn) + ": lr must be finite");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     int rc = ensure_device(h, stream);      // uploads host-side parameters first if they are the newer ones
     if (rc != ROCKET_OK) return rc;
@@ -965,12 +966,26 @@ extern "C" int rocket_sgd_update(rocket_kernels *h, const float *grad_w_dev, con
         // an earlier update ran on another stream (which may no longer exist): order this one after it
         RK_HIP(hipDeviceSynchronize());
     }
-    if (rk_launch_sgd_update(h, grad_w_dev, grad_b_dev, lr, recentre, stream) != ROCKET_OK)
+    if ((norm_dev ? rk_launchers().sgd_update_clipped(h, grad_w_dev, grad_b_dev, lr, recentre, norm_dev, stream)
+                  : rk_launch_sgd_update(h, grad_w_dev, grad_b_dev, lr, recentre, stream)) != ROCKET_OK)
         return rk_fail(ROCKET_EHIP, "launch of the update kernel failed");
     h->host_stale = true;
     h->update_stream = hip_stream;
     h->mr_groups = 0;              // trained weights are no longer the predetermined set
     return ROCKET_OK;
+}
+
+extern "C" int rocket_sgd_update(rocket_kernels *h, const float *grad_w_dev, const float *grad_b_dev, float lr,
+                                 int recentre, void *hip_stream)
+{
+    return sgd_update_impl("rocket_sgd_update", h, grad_w_dev, grad_b_dev, lr, recentre, nullptr, hip_stream);
+}
+
+extern "C" int rocket_sgd_update_clipped(rocket_kernels *h, const float *grad_w_dev, const float *grad_b_dev, float lr,
+                                         int recentre, const double *norm_dev, void *hip_stream)
+{
+    if (!norm_dev) return rk_fail(ROCKET_EINVAL, "rocket_sgd_update_clipped: NULL norm");
+    return sgd_update_impl("rocket_sgd_update_clipped", h, grad_w_dev, grad_b_dev, lr, recentre, norm_dev, hip_stream);
 }
 
 // layout of the training workspace: [transform / backward workspace][features][upstream gradient]

@@ -259,6 +259,9 @@ struct RkLaunchers {
                            float *grad_b, void *stream) = nullptr;
     // the sum of those rows
     int (*sum_groups)(const rocket_kernels *h, const RkGroups &groups, const float *partial, float *grad_w, float *grad_b, void *stream) = nullptr;
+    // rocket_train.hip: rk_launch_sgd_update with lr times the coefficient norm[1] (norm may be null)
+    int (*sgd_update_clipped)(const rocket_kernels *h, const float *gw, const float *gb, float lr, int recentre, const double *norm,
+                              void *stream) = nullptr;
 };
 RkLaunchers &rk_launchers();      // rocket_api.hip
 // rocket_api.hip: offsets, sets, job plan, padded row geometry; returns ROCKET_OK or an error

@@ -5,7 +5,8 @@
 //
 //   rk_mse_grad   : G[b][i] = (2/B) (pred_b - y_b) coef[i]  and  loss = (1/B) sum_b (pred_b - y_b)^2
 //   rk_sgd_update : w <- w - lr*gw, b <- b - lr*gb on the handle's device parameters, with an
-//                   optional re-centring of every (kernel, channel) weight row
+//                   optional re-centring of every (kernel, channel) weight row; with the norm of rocket_grad_norm the
+//                   coefficient that clips the gradients is applied to lr here, so clipped gradients are never stored
 #include <hip/hip_runtime.h>
 
 #include "rocket_internal.hpp"
@@ -36,8 +37,10 @@ constexpr int kUpdateRows = 9;       // sampled kernels have no more channels
 constexpr int kUpdateKernels = 28;   // of a workgroup
 __global__ __launch_bounds__(kUpdateRows * kUpdateKernels) void rk_sgd_update(RkKernelRec *__restrict__ recs, float *__restrict__ weights,
                                                                               const float *__restrict__ gw, const float *__restrict__ gb,
-                                                                              int K, float lr, int recentre)
+                                                                              int K, float rate, const double *__restrict__ norm,
+                                                                              int recentre)
 {
+    const float lr = norm ? static_cast<float>(static_cast<double>(rate) * norm[1]) : rate;
     const int kl = static_cast<int>(threadIdx.x) / kUpdateRows, row0 = static_cast<int>(threadIdx.x) - kl * kUpdateRows;
     const int k = static_cast<int>(blockIdx.x) * kUpdateKernels + kl;
     if (k >= K) return;
@@ -70,11 +73,18 @@ int rk_launch_mse_grad(const double *pred, const float *targets, const double *c
     return hipGetLastError() == hipSuccess ? ROCKET_OK : ROCKET_EHIP;
 }
 
-int rk_launch_sgd_update(const rocket_kernels *h, const float *gw, const float *gb, float lr, int recentre,
-                         void *stream_ptr)
+static int launch_sgd_update(const rocket_kernels *h, const float *gw, const float *gb, float lr, int recentre, const double *norm,
+                             void *stream_ptr)
 {
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     hipLaunchKernelGGL(rk_sgd_update, dim3(static_cast<unsigned>((h->K + kUpdateKernels - 1) / kUpdateKernels)),
-                       dim3(kUpdateRows * kUpdateKernels), 0, stream, const_cast<RkKernelRec *>(h->d_rec), h->d_weights, gw, gb, h->K, lr, recentre);
+                       dim3(kUpdateRows * kUpdateKernels), 0, stream, const_cast<RkKernelRec *>(h->d_rec), h->d_weights, gw, gb, h->K, lr, norm, recentre);
     return hipGetLastError() == hipSuccess ? ROCKET_OK : ROCKET_EHIP;
 }
+
+int rk_launch_sgd_update(const rocket_kernels *h, const float *gw, const float *gb, float lr, int recentre, void *stream)
+{
+    return launch_sgd_update(h, gw, gb, lr, recentre, nullptr, stream);
+}
+
+[[maybe_unused]] static const bool kEntered = (rk_launchers().sgd_update_clipped = launch_sgd_update, true);

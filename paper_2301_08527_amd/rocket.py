@@ -11,6 +11,7 @@ import os
 import numpy as np
 
 ROCKET_F_MAX, ROCKET_F_PPV, ROCKET_F_SOFTPPV = 1, 2, 4
+ROCKET_F32, ROCKET_BF16, ROCKET_F16 = 0, 1, 2
 ROCKET_OK, ROCKET_EINVAL, ROCKET_ENOMEM, ROCKET_EHIP, ROCKET_ESHAPE, ROCKET_EWORKSPACE = 0, -1, -2, -3, -4, -5
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -26,6 +27,10 @@ EXPORTS = [
     "rocket_ridge_workspace_bytes", "rocket_ridge_fit", "rocket_ridge_predict", "rocket_infer",
     "rocket_mse_grad", "rocket_sgd_update", "rocket_train_workspace_bytes", "rocket_train_step",
     "rocket_kernels_subset",
+    "rocket_layer_norm_workspace_bytes", "rocket_layer_norm", "rocket_layer_norm_backward",
+    "rocket_grad_workspace_bytes", "rocket_grad_norm", "rocket_grad_clip", "rocket_sgd_tensors", "rocket_sgd_update_clipped",
+    "rocket_infer_normed_workspace_bytes", "rocket_infer_normed", "rocket_train_normed_workspace_bytes",
+    "rocket_train_step_normed",
     "rocket_minirocket_kernels", "rocket_minirocket_fit_workspace_bytes", "rocket_minirocket_fit_bias",
     "rocket_minirocket_workspace_bytes", "rocket_minirocket_transform", "rocket_minirocket_transform_u8",
     "rocket_minirocket_jobs_view_get",
@@ -95,6 +100,23 @@ def load_library():
     lib.rocket_train_step.argtypes = [vp, vp, C.c_int, i32, u32, f32, f32, vp, vp, vp, f32, C.c_int, vp, vp,
                                       C.c_size_t, vp]
     lib.rocket_kernels_subset.argtypes = [vp, vp, i32, C.POINTER(vp)]
+    f64, sz = C.c_double, C.c_size_t
+    lib.rocket_layer_norm_workspace_bytes.argtypes = [i32, i32, i32, C.c_int]
+    lib.rocket_layer_norm_workspace_bytes.restype = sz
+    lib.rocket_layer_norm.argtypes = [vp, i32, i32, i32, i32, vp, vp, f32, vp, vp, vp, vp, sz, vp]
+    lib.rocket_layer_norm_backward.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.rocket_grad_workspace_bytes.argtypes = [vp, i32]
+    lib.rocket_grad_workspace_bytes.restype = sz
+    lib.rocket_grad_norm.argtypes = [vp, i32, f64, vp, vp, sz, vp]
+    lib.rocket_grad_clip.argtypes = [vp, vp, i32, f64, vp, vp, sz, vp]
+    lib.rocket_sgd_tensors.argtypes = [vp, vp, vp, i32, f64, vp, vp]
+    lib.rocket_sgd_update_clipped.argtypes = [vp, vp, vp, f32, C.c_int, vp, vp]
+    for name in ("rocket_infer_normed_workspace_bytes", "rocket_train_normed_workspace_bytes"):
+        getattr(lib, name).argtypes = [vp, i32, u32]
+        getattr(lib, name).restype = sz
+    lib.rocket_infer_normed.argtypes = [vp, vp, C.c_int, i32, u32, f32, f32, vp, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+    lib.rocket_train_step_normed.argtypes = [vp, vp, C.c_int, i32, u32, f32, f32, vp, vp, f32, vp, vp, vp, f32, C.c_int, f64,
+                                             vp, vp, vp, sz, vp]
     lib.rocket_minirocket_kernels.argtypes = [u64, i32, i32, i32, C.POINTER(vp)]
     lib.rocket_minirocket_fit_workspace_bytes.argtypes = [vp, i32]
     lib.rocket_minirocket_fit_workspace_bytes.restype = C.c_size_t
@@ -470,6 +492,286 @@ def rocket_train_step(kernels, x, feature_mask, coef, intercept, targets, lr, la
         coef.data_ptr(), intercept.data_ptr(), targets.data_ptr(), lr, int(bool(recentre)), loss.data_ptr(),
         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(torch, stream)))
     return loss
+
+
+# ------------------------------------------------------------------ layer norm, many tensors
+
+def _type_code(torch, dtype):
+    return {torch.float32: ROCKET_F32, torch.bfloat16: ROCKET_BF16, torch.float16: ROCKET_F16}.get(dtype)
+
+
+def _current(torch, stream, *tensors):
+    """Refuses tensors, or a stream, of another device than the current one."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise RocketError(ROCKET_EINVAL, "a tensor on %s: the current device is cuda:%d" % (t.device, here))
+    if stream is not None and stream.device.index != here:
+        raise RocketError(ROCKET_EINVAL, "a stream of %s: the current device is cuda:%d" % (stream.device, here))
+
+
+def _empty(torch, shape, dtype, stream):
+    """Memory of the current device that belongs to the stream it will be used on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _scratch(torch, need, workspace, stream):
+    """(address, bytes) of the workspace, and the tensor to keep until the call was made."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = _empty(torch, need, torch.uint8, stream)
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise RocketError(ROCKET_EWORKSPACE, "workspace must be a contiguous CUDA tensor")
+    else:
+        _current(torch, stream, workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _fits(t, like, dtype, name):
+    """An output or input that has to have a shape and a type."""
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(like)):
+        raise RocketError(ROCKET_EINVAL, "%s must be a contiguous %s CUDA tensor of shape %s" % (name, dtype, tuple(like)))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _norm_sizes(torch, x, planes):
+    code = _type_code(torch, x.dtype)
+    if not (x.is_cuda and code is not None and x.is_contiguous() and x.dim() == 2):
+        raise RocketError(ROCKET_EINVAL, "x must be a contiguous float32, bfloat16 or float16 CUDA tensor (rows, planes * n)")
+    rows, wide = x.shape
+    if planes < 1 or rows < 1 or wide < 1 or wide % planes:
+        raise RocketError(ROCKET_ESHAPE, "x (%d, %d) is not rows of %d planes" % (rows, wide, planes))
+    return code, rows, wide // planes
+
+
+def rocket_layer_norm_workspace_bytes(rows, planes, n, backward=True):
+    return int(load_library().rocket_layer_norm_workspace_bytes(rows, planes, n, int(bool(backward))))
+
+
+def rocket_layer_norm(x, weight=None, bias=None, eps=1e-5, planes=1, y=None, mean=None, rstd=None, workspace=None, stream=None):
+    """x: (rows, planes * n), float32, bfloat16 or float16; weight, bias: float32 (planes * n,).  Every plane of a row is
+    normalised by itself.  Returns y (x's type); mean and rstd, float32 (rows, planes), are written for the backward pass
+    where both are given."""
+    torch = _torch()
+    code, rows, n = _norm_sizes(torch, x, planes)
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _fits(t, (planes * n,), torch.float32, name)
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is not None:
+            _fits(t, (rows, planes), torch.float32, name)
+    if y is not None:
+        _fits(y, x.shape, x.dtype, "y")
+    _current(torch, stream, x, weight, bias, y, mean, rstd)
+    if y is None:
+        y = _empty(torch, x.shape, x.dtype, stream)
+    ws, size, keep = _scratch(torch, rocket_layer_norm_workspace_bytes(rows, planes, n, False), workspace, stream)
+    _check(load_library().rocket_layer_norm(x.data_ptr(), code, rows, planes, n, _ptr(weight), _ptr(bias), eps, y.data_ptr(),
+                                            _ptr(mean), _ptr(rstd), ws, size, _stream_ptr(torch, stream)))
+    return y
+
+
+def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, grad_x=None, grad_weight=None, grad_bias=None,
+                               workspace=None, stream=None):
+    """Returns (grad_x of x's type, grad_weight, grad_bias float32 (planes * n,)).  grad_x may be grad_y."""
+    torch = _torch()
+    code, rows, n = _norm_sizes(torch, x, planes)
+    _fits(grad_y, x.shape, x.dtype, "grad_y")
+    _fits(mean, (rows, planes), torch.float32, "mean")
+    _fits(rstd, (rows, planes), torch.float32, "rstd")
+    if weight is not None:
+        _fits(weight, (planes * n,), torch.float32, "weight")
+    if grad_x is not None:
+        _fits(grad_x, x.shape, x.dtype, "grad_x")
+    for t, name in ((grad_weight, "grad_weight"), (grad_bias, "grad_bias")):
+        if t is not None:
+            _fits(t, (planes * n,), torch.float32, name)
+    _current(torch, stream, x, grad_y, mean, rstd, weight, grad_x, grad_weight, grad_bias)
+    if grad_x is None:
+        grad_x = _empty(torch, x.shape, x.dtype, stream)
+    if grad_weight is None:
+        grad_weight = _empty(torch, (planes * n,), torch.float32, stream)
+    if grad_bias is None:
+        grad_bias = _empty(torch, (planes * n,), torch.float32, stream)
+    ws, size, keep = _scratch(torch, rocket_layer_norm_workspace_bytes(rows, planes, n, True), workspace, stream)
+    _check(load_library().rocket_layer_norm_backward(
+        x.data_ptr(), grad_y.data_ptr(), code, rows, planes, n, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), grad_x.data_ptr(),
+        grad_weight.data_ptr(), grad_bias.data_ptr(), ws, size, _stream_ptr(torch, stream)))
+    return grad_x, grad_weight, grad_bias
+
+
+class Tensors:
+    """A list of CUDA tensors as the library reads it (rocket_tensor records).  It keeps the tensors alive and holds the
+    addresses they have when it is made: make a new one after a tensor's memory was replaced."""
+    _RECORD = np.dtype([("data", np.uint64), ("count", np.int64), ("dtype", np.int32), ("reserved", np.int32)])
+
+    def __init__(self, tensors):
+        torch = _torch()
+        self.tensors = list(tensors)
+        codes = {torch.float32: ROCKET_F32, torch.bfloat16: ROCKET_BF16, torch.float16: ROCKET_F16}
+        if not self.tensors:
+            raise RocketError(ROCKET_EINVAL, "a list holds one tensor at least")
+        self.device = self.tensors[0].device
+        records = []
+        for i, t in enumerate(self.tensors):
+            code = codes.get(t.dtype)
+            if code is None or not t.is_cuda or not t.is_contiguous() or t.device != self.device:
+                raise RocketError(ROCKET_EINVAL, "tensor %d must be a contiguous float32, bfloat16 or float16 CUDA tensor on %s"
+                                  % (i, self.device))
+            records.append((t.data_ptr(), t.numel(), code, 0))
+        self._records = np.array(records, dtype=self._RECORD)
+        self.address = self._records.ctypes.data
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def rocket_tensors(tensors):
+    """The list that rocket_grad_norm, rocket_grad_clip and rocket_sgd_tensors take: made once where a program keeps its
+    tensors (they also take a plain list, and then make it at every call)."""
+    return tensors if isinstance(tensors, Tensors) else Tensors(tensors)
+
+
+def rocket_grad_workspace_bytes(grads):
+    grads = rocket_tensors(grads)
+    return int(load_library().rocket_grad_workspace_bytes(grads.address, len(grads)))
+
+
+def _norm_out(torch, norm, stream):
+    if norm is None:
+        return _empty(torch, 2, torch.float64, stream)
+    _fits(norm, (2,), torch.float64, "norm")
+    return norm
+
+
+def rocket_grad_norm(grads, max_norm=float("inf"), norm=None, workspace=None, stream=None):
+    """Returns norm, float64 (2,): the norm over all values of all gradients, and the coefficient min(1, max_norm / norm)."""
+    torch = _torch()
+    grads = rocket_tensors(grads)
+    _current(torch, stream, grads, norm)
+    norm = _norm_out(torch, norm, stream)
+    need = 0 if workspace is not None else rocket_grad_workspace_bytes(grads)
+    ws, size, keep = _scratch(torch, need, workspace, stream)
+    _check(load_library().rocket_grad_norm(grads.address, len(grads), max_norm, norm.data_ptr(), ws, size, _stream_ptr(torch, stream)))
+    return norm
+
+
+def _same_length(a, b):
+    if len(a) != len(b):
+        raise RocketError(ROCKET_ESHAPE, "lists of %d and %d tensors" % (len(a), len(b)))
+
+
+def rocket_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
+    """Scales the gradients (in place, or into `out`) so that their norm is at most max_norm.  Returns norm as
+    rocket_grad_norm does."""
+    torch = _torch()
+    grads = rocket_tensors(grads)
+    if out is not None:
+        out = rocket_tensors(out)
+        _same_length(grads, out)
+    _current(torch, stream, grads, out, norm)
+    norm = _norm_out(torch, norm, stream)
+    need = 0 if workspace is not None else rocket_grad_workspace_bytes(grads)
+    ws, size, keep = _scratch(torch, need, workspace, stream)
+    _check(load_library().rocket_grad_clip(grads.address, None if out is None else out.address, len(grads), max_norm,
+                                           norm.data_ptr(), ws, size, _stream_ptr(torch, stream)))
+    return norm
+
+
+def rocket_sgd_tensors(params, grads, lr, norm=None, out=None, stream=None):
+    """params (or `out`) = params - lr * norm[1] * grads; norm as rocket_grad_norm returns it, or None: not clipped."""
+    torch = _torch()
+    params, grads = rocket_tensors(params), rocket_tensors(grads)
+    _same_length(params, grads)
+    if out is not None:
+        out = rocket_tensors(out)
+        _same_length(params, out)
+    if norm is not None:
+        _fits(norm, (2,), torch.float64, "norm")
+    _current(torch, stream, params, grads, out, norm)
+    _check(load_library().rocket_sgd_tensors(params.address, grads.address, None if out is None else out.address, len(params), lr,
+                                             _ptr(norm), _stream_ptr(torch, stream)))
+
+
+def rocket_sgd_update_clipped(kernels, grad_w, grad_b, lr, norm, recentre=False, stream=None):
+    """rocket_sgd_update with lr * norm[1]; norm as rocket_grad_norm returns it."""
+    torch = _torch()
+    _fits(grad_w, (kernels.total_weights,), torch.float32, "grad_w")
+    _fits(grad_b, (kernels.K,), torch.float32, "grad_b")
+    _fits(norm, (2,), torch.float64, "norm")
+    _current(torch, stream, grad_w, grad_b, norm)
+    _check(load_library().rocket_sgd_update_clipped(kernels.handle, grad_w.data_ptr(), grad_b.data_ptr(), lr, int(bool(recentre)),
+                                                    norm.data_ptr(), _stream_ptr(torch, stream)))
+
+
+def _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept):
+    if not (x.is_cuda and x.dtype in (torch.float32, torch.uint8) and x.is_contiguous() and x.dim() == 3):
+        raise RocketError(ROCKET_EINVAL, "x must be a contiguous float32 or uint8 CUDA tensor of shape (B, C, L)")
+    if x.shape[1] != kernels.C or x.shape[2] != kernels.L:
+        raise RocketError(ROCKET_ESHAPE, "x does not match the kernels' (C, L)")
+    p = rocket_num_features(feature_mask) * kernels.K
+    for t, name in ((norm_weight, "norm_weight"), (norm_bias, "norm_bias")):
+        if t is not None:
+            _fits(t, (p,), torch.float32, name)
+    _fits(coef, (p,), torch.float64, "coef")
+    _fits(intercept, (1,), torch.float64, "intercept")
+    return x.shape[0], p
+
+
+def rocket_infer_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, eps=1e-5, lam=10.0, shift=-3.0,
+                        features=None, workspace=None, stream=None):
+    """rocket_infer with a layer norm of every feature plane before the head.  norm_weight, norm_bias: float32 (F*K,) or
+    None.  Returns (pred float64 (B,), the normalised features float32 (B, F*K))."""
+    torch = _torch()
+    B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept)
+    if features is not None:
+        _fits(features, (B, p), torch.float32, "features")
+    _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, features)
+    if features is None:
+        features = _empty(torch, (B, p), torch.float32, stream)
+    pred = _empty(torch, B, torch.float64, stream)
+    need = int(load_library().rocket_infer_normed_workspace_bytes(kernels.handle, B, feature_mask))
+    ws, size, keep = _scratch(torch, need, workspace, stream)
+    _check(load_library().rocket_infer_normed(
+        kernels.handle, x.data_ptr(), int(x.dtype == torch.uint8), B, feature_mask, lam, shift, _ptr(norm_weight), _ptr(norm_bias), eps,
+        coef.data_ptr(), intercept.data_ptr(), features.data_ptr(), pred.data_ptr(), ws, size, _stream_ptr(torch, stream)))
+    return pred, features
+
+
+def rocket_infer_normed_workspace_bytes(kernels, B, feature_mask):
+    return int(load_library().rocket_infer_normed_workspace_bytes(kernels.handle, B, feature_mask))
+
+
+def rocket_train_normed_workspace_bytes(kernels, B, feature_mask):
+    return int(load_library().rocket_train_normed_workspace_bytes(kernels.handle, B, feature_mask))
+
+
+def rocket_train_step_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, targets, lr, max_norm=float("inf"),
+                             eps=1e-5, lam=10.0, shift=-3.0, recentre=False, norm=None, workspace=None, stream=None):
+    """One clipped gradient-descent step on the kernels and, in place, on norm_weight and norm_bias (float32 (F*K,)).
+    Returns (loss before the update, float64 (1,), norm as rocket_grad_norm returns it)."""
+    torch = _torch()
+    B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept)
+    if norm_weight is None or norm_bias is None:
+        raise RocketError(ROCKET_EINVAL, "norm_weight and norm_bias are trained: both are needed")
+    _fits(targets, (B,), torch.float32, "targets")
+    _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, targets, norm)
+    norm = _norm_out(torch, norm, stream)
+    loss = _empty(torch, 1, torch.float64, stream)
+    need = rocket_train_normed_workspace_bytes(kernels, B, feature_mask)
+    ws, size, keep = _scratch(torch, need, workspace, stream)
+    _check(load_library().rocket_train_step_normed(
+        kernels.handle, x.data_ptr(), int(x.dtype == torch.uint8), B, feature_mask, lam, shift, norm_weight.data_ptr(),
+        norm_bias.data_ptr(), eps, coef.data_ptr(), intercept.data_ptr(), targets.data_ptr(), lr, int(bool(recentre)), max_norm,
+        loss.data_ptr(), norm.data_ptr(), ws, size, _stream_ptr(torch, stream)))
+    return loss, norm
 
 
 def rocket_kernels_subset(kernels, index):
