@@ -53,3 +53,21 @@ __device__ __forceinline__ void rk_store(T *p, int64_t left, const float (&v)[kP
             if (i < left) p[i] = static_cast<T>(v[i]);
     }
 }
+
+// N fp32 values from p on, as far as the first `left` of them exist (the others stay as they are)
+template <int N>
+__device__ __forceinline__ void rk_load_f32(const float *p, int64_t left, float (&v)[N])
+{
+    if (left >= N) {
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const auto q = reinterpret_cast<const RkSlot<float> *>(p + k)->v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[k + i] = q[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) v[i] = p[i];
+    }
+}

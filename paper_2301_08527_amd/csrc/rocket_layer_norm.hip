@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "rocket_elements.hpp"
 #include "rocket_internal.hpp"
@@ -20,6 +21,250 @@
 namespace {
 
 constexpr int kNormThreads = 256;
+
+// ------------------------------------------------------------------ sums over lanes
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float rn_dpp(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+
+// Sum over 16 or 64 neighbouring lanes, the same bits on each of them: rotations within the rows of 16 lanes, then the
+// rows' sums one after the other into the last row.
+template <int LANES>
+__device__ __forceinline__ float rn_lanes_sum(float v)
+{
+    static_assert(LANES == 16 || LANES == 64, "a row of lanes or a wavefront");
+    v += rn_dpp<0x128, 0xf>(v);       // row_ror:8, 4, 2, 1
+    v += rn_dpp<0x124, 0xf>(v);
+    v += rn_dpp<0x122, 0xf>(v);
+    v += rn_dpp<0x121, 0xf>(v);
+    if constexpr (LANES == 64) {
+        v += rn_dpp<0x142, 0xa>(v);   // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+        v += rn_dpp<0x143, 0xc>(v);
+        v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    }
+    return v;
+}
+
+// Count, mean and sum of squared distances from it of some values of a row, the mean as shift + rest: two parts whose sum has
+// more than 32 bits, so that x - shift - rest is right to the last bits however far from zero the row lies.
+struct Moments {
+    float count, shift, rest, m2;
+};
+
+// Of all values that the LANES lanes of a row hold in `raw`.  `left[s]` values of slot s exist, `n` of all lanes.
+template <class T, int SLOTS>
+using Held = typename RkSlot<T>::V[SLOTS];
+
+template <class T, int LANES, int SLOTS>
+__device__ __forceinline__ Moments rn_moments(const Held<T, SLOTS> &raw, int i0, int step, int n, float count)
+{
+    constexpr int N = kPerLoad<T>;
+    float s = 0.f;        // values that do not exist are zeros
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k)
+#pragma unroll
+        for (int q = 0; q < N; ++q) s += static_cast<float>(raw[k][q]);
+    const float shift = rn_lanes_sum<LANES>(s) / count;
+    float d1 = 0.f, d2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+        const int left = n - (i0 + k * step);
+        if (left >= N) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const float d = static_cast<float>(raw[k][q]) - shift;
+                d1 += d;
+                d2 = fmaf(d, d, d2);
+            }
+        } else if (left > 0) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const float d = q < left ? static_cast<float>(raw[k][q]) - shift : 0.f;
+                d1 += d;
+                d2 = fmaf(d, d, d2);
+            }
+        }
+    }
+    d1 = rn_lanes_sum<LANES>(d1);
+    d2 = rn_lanes_sum<LANES>(d2);
+    const float rest = d1 / count;
+    const float m2 = fmaf(-rest, d1, d2);
+    return {count, shift, rest, m2 < 0.f ? 0.f : m2};      // NaN stays
+}
+
+// Moments of the values of up to 16 parts, of which lane l of every row of 16 lanes holds part l (count 0: none): distances of
+// the parts' means from the first one's, weighted by their counts.
+__device__ __forceinline__ Moments rn_join(const Moments &part, float n)
+{
+    const float shift = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, part.shift), 0));
+    const bool some = part.count > 0.f;
+    const float off = some ? (part.shift - shift) + part.rest : 0.f;
+    const float rest = rn_lanes_sum<16>(part.count * off) / n;
+    const float apart = off - rest;
+    return {n, shift, rest, rn_lanes_sum<16>(some ? fmaf(part.count * apart, apart, part.m2) : 0.f)};
+}
+
+template <class T, int SLOTS>
+__device__ __forceinline__ void rn_hold(Held<T, SLOTS> &raw, const T *src, int i0, int step, int n)
+{
+    constexpr int N = kPerLoad<T>;
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+        const int i = i0 + k * step;
+        if (i + N <= n) {
+            raw[k] = reinterpret_cast<const RkSlot<T> *>(src + i)->v;
+        } else {
+#pragma unroll
+            for (int q = 0; q < N; ++q) raw[k][q] = i + q < n ? src[i + q] : static_cast<T>(0.f);
+        }
+    }
+}
+
+template <class T, int SLOTS>
+__device__ __forceinline__ void rn_write(const Held<T, SLOTS> &raw, T *dst, int i0, int step, int n, const Moments &m, float r, const float *weight,
+                                         const float *bias)
+{
+    constexpr int N = kPerLoad<T>;
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+        const int i = i0 + k * step;
+        if (i >= n) break;
+        float v[N], w[N], b[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) w[q] = 1.f, b[q] = 0.f;
+        if (weight) rk_load_f32<N>(weight + i, n - i, w);
+        if (bias) rk_load_f32<N>(bias + i, n - i, b);
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = fmaf(((static_cast<float>(raw[k][q]) - m.shift) - m.rest) * r, w[q], b[q]);
+        rk_store(dst + i, n - i, v);
+    }
+}
+
+// n as a float: exact up to 2^24, and a rounding of 2^-25 of the mean of squares beyond
+__device__ __forceinline__ float rn_rstd(const Moments &m, float eps) { return 1.f / sqrtf(m.m2 / m.count + eps); }
+
+// A row lies in the registers of LANES lanes, SLOTS loads of 16 bytes in each (as loaded: 16-bit values take half the registers),
+// so x is read once.  Two passes over the registers give the mean and the distances from it; up to 64 lanes meet by lane
+// rotations alone, more lanes once through LDS, where the wavefronts' own means and sums of squares are joined.
+template <class T, int LANES, int SLOTS>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int64_t R, int planes, int n, const float *__restrict__ weight,
+                                                                        const float *__restrict__ bias, float eps, T *y,
+                                                                        float *__restrict__ mean, float *__restrict__ rstd)
+{
+    constexpr int N = kPerLoad<T>, kRows = LANES < 256 ? 256 / LANES : 1;
+    __shared__ float4 lds[LANES > 64 ? 16 : 1];
+    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1), i0 = lane * N, step = LANES * N;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / LANES;
+    if (row >= R) return;
+    Held<T, SLOTS> raw;
+    rn_hold<T, SLOTS>(raw, x + row * n, i0, step, n);
+    Moments m;
+    if constexpr (LANES <= 64) {
+        m = rn_moments<T, LANES, SLOTS>(raw, i0, step, n, static_cast<float>(n));
+    } else {
+        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+        int count = 0;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) count += min(max(n - (k * step + wave * 64 * N), 0), 64 * N);
+        const Moments own = rn_moments<T, 64, SLOTS>(raw, i0, step, n, static_cast<float>(max(count, 1)));
+        if (static_cast<int>(threadIdx.x) < 16) lds[threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[wave] = make_float4(static_cast<float>(count), own.shift, own.rest, own.m2);
+        __syncthreads();
+        const float4 part = lds[threadIdx.x & 15];
+        m = rn_join({part.x, part.y, part.z, part.w}, static_cast<float>(n));
+    }
+    const float r = rn_rstd(m, eps);
+    const int64_t w0 = row % planes * n;
+    rn_write<T, SLOTS>(raw, y + row * n, i0, step, n, m, r, weight ? weight + w0 : nullptr, bias ? bias + w0 : nullptr);
+    if (mean && lane == 0) {
+        mean[row] = m.shift + m.rest;
+        rstd[row] = r;
+    }
+}
+
+// Longer rows: moments of parts of a row, one workgroup each, then each part again with those of its row joined.  At most kMostParts
+// parts to a row; a part is `length` values, in pieces of kPart that a workgroup holds.  grid (parts, R up to 2^15 and on)
+constexpr int kMostParts = 64, kPartSlots = 4;
+template <class T>
+constexpr int kPart = kNormThreads * kPartSlots * kPerLoad<T>;
+
+template <class T>
+__global__ __launch_bounds__(kNormThreads) void rn_forward_parts(const T *x, int64_t R, int n, int length, float4 *__restrict__ moments)
+{
+    constexpr int N = kPerLoad<T>;
+    __shared__ float4 lds[16];
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    for (int64_t row = blockIdx.y; row < R; row += gridDim.y) {
+        const int from = static_cast<int>(blockIdx.x) * length, to = min(n - from, length) + from;
+        Moments m = {0.f, 0.f, 0.f, 0.f};
+        for (int64_t at = from; at < to; at += kPart<T>) {
+            const int some = static_cast<int>(min(static_cast<int64_t>(to) - at, static_cast<int64_t>(kPart<T>)));
+            Held<T, kPartSlots> raw;
+            rn_hold<T, kPartSlots>(raw, x + row * n + at, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some);
+            int count = 0;
+#pragma unroll
+            for (int k = 0; k < kPartSlots; ++k) count += min(max(some - (k * kNormThreads * N + wave * 64 * N), 0), 64 * N);
+            const Moments own = rn_moments<T, 64, kPartSlots>(raw, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some, static_cast<float>(max(count, 1)));
+            __syncthreads();      // the last piece has been read
+            if (static_cast<int>(threadIdx.x) < 16) lds[threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) lds[wave] = make_float4(static_cast<float>(count), own.shift, own.rest, own.m2);
+            if (threadIdx.x == 0) lds[4] = make_float4(m.count, m.shift, m.rest, m.m2);      // what came before
+            __syncthreads();
+            const float4 part = lds[threadIdx.x & 15];
+            m = rn_join({part.x, part.y, part.z, part.w}, m.count + static_cast<float>(some));
+        }
+        if (threadIdx.x == 0) moments[row * gridDim.x + blockIdx.x] = make_float4(m.count, m.shift, m.rest, m.m2);
+    }
+}
+
+// The moments of a row from those of its parts, 16 at a time.
+__device__ __forceinline__ Moments rn_row_moments(const float4 *moments, int parts)
+{
+    Moments m = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; p += 15) {
+        const int l = static_cast<int>(threadIdx.x) & 15;
+        const bool some = l > 0 && p + l - 1 < parts;
+        const float4 part = some ? moments[p + l - 1] : make_float4(l == 0 ? m.count : 0.f, m.shift, m.rest, m.m2);
+        const float count = rn_lanes_sum<16>(part.x);
+        if (p == 0) {       // nothing before: the first part takes its place, so that the shift is one of the row's means
+            const float4 first = moments[0];
+            const Moments mine = {l == 0 ? 0.f : part.x, l == 0 ? first.y : part.y, l == 0 ? 0.f : part.z, l == 0 ? 0.f : part.w};
+            m = rn_join(mine, count);
+        } else {
+            m = rn_join({part.x, part.y, part.z, part.w}, count);
+        }
+    }
+    return m;
+}
+
+template <class T>
+__global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int64_t R, int planes, int n, int length, int parts,
+                                                                 const float4 *__restrict__ moments, const float *__restrict__ weight,
+                                                                 const float *__restrict__ bias, float eps, T *y, float *__restrict__ mean,
+                                                                 float *__restrict__ rstd)
+{
+    constexpr int N = kPerLoad<T>;
+    for (int64_t row = blockIdx.y; row < R; row += gridDim.y) {
+        const Moments m = rn_row_moments(moments + row * parts, parts);
+        const float r = rn_rstd(m, eps);
+        const int64_t w0 = row % planes * n;
+        const int64_t from = static_cast<int64_t>(blockIdx.x) * kPart<T>;
+        const int some = static_cast<int>(min(static_cast<int64_t>(n) - from, static_cast<int64_t>(kPart<T>)));
+        Held<T, kPartSlots> raw;
+        rn_hold<T, kPartSlots>(raw, x + row * n + from, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some);
+        rn_write<T, kPartSlots>(raw, y + row * n + from, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some, m, r,
+                                weight ? weight + w0 + from : nullptr, bias ? bias + w0 + from : nullptr);
+        if (mean && blockIdx.x == 0 && threadIdx.x == 0) {
+            mean[row] = m.shift + m.rest;
+            rstd[row] = r;
+        }
+    }
+}
 
 // Sums of N values over the workgroup, the same on every lane.
 template <int N, class S>
@@ -39,58 +284,6 @@ __device__ __forceinline__ void rn_sum(S (&v)[N], S *lds)
         S s = 0;
         for (int w = 0; w < kNormThreads / 64; ++w) s += lds[w * N + i];
         v[i] = s;
-    }
-}
-
-// One workgroup per row, three passes over it.
-template <class T>
-__global__ __launch_bounds__(kNormThreads) void rn_forward(const T *x, int64_t R, int planes, int n, const float *__restrict__ weight,
-                                                           const float *__restrict__ bias, float eps, T *y, float *__restrict__ mean,
-                                                           float *__restrict__ rstd)
-{
-    constexpr int N = kPerLoad<T>;
-    __shared__ double lds[kNormThreads / 64];
-    for (int64_t row = blockIdx.x; row < R; row += gridDim.x) {
-        const T *src = x + row * n;
-        T *dst = y + row * n;
-        const int64_t w0 = row % planes * n;
-        float v[N], wt[N], bs[N];
-        double s[1] = {0.0};
-        for (int i = static_cast<int>(threadIdx.x) * N; i < n; i += kNormThreads * N) {
-            rk_load(src + i, n - i, v);
-#pragma unroll
-            for (int q = 0; q < N; ++q) s[0] += static_cast<double>(v[q]);
-        }
-        rn_sum(s, lds);
-        const double m = s[0] / n;
-        s[0] = 0.0;
-        for (int i = static_cast<int>(threadIdx.x) * N; i < n; i += kNormThreads * N) {
-            rk_load(src + i, n - i, v);
-#pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const double d = i + q < n ? static_cast<double>(v[q]) - m : 0.0;
-                s[0] += d * d;
-            }
-        }
-        rn_sum(s, lds);
-        const float hi = static_cast<float>(m), lo = static_cast<float>(m - static_cast<double>(hi));
-        const float r = static_cast<float>(1.0 / sqrt(s[0] / n + static_cast<double>(eps)));
-        for (int i = static_cast<int>(threadIdx.x) * N; i < n; i += kNormThreads * N) {
-            rk_load(src + i, n - i, v);
-#pragma unroll
-            for (int q = 0; q < N; ++q) wt[q] = 1.f, bs[q] = 0.f;
-            for (int q = 0; q < N; ++q) {
-                if (weight && i + q < n) wt[q] = weight[w0 + i + q];
-                if (bias && i + q < n) bs[q] = bias[w0 + i + q];
-            }
-#pragma unroll
-            for (int q = 0; q < N; ++q) v[q] = fmaf(((v[q] - hi) - lo) * r, wt[q], bs[q]);
-            rk_store(dst + i, n - i, v);
-        }
-        if (mean && threadIdx.x == 0) {
-            mean[row] = hi;
-            rstd[row] = r;
-        }
     }
 }
 
@@ -180,6 +373,25 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_finish(const float *
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// How a row is held: in registers as long as 8 loads of 1,024 lanes hold it, else in parts.
+struct ForwardPlan {
+    int64_t R;
+    int parts = 0, length = 0;
+    ForwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes)
+    {
+        const int64_t per = 16 / static_cast<int64_t>(rk_type_bytes(dtype));
+        if (n <= 8 * 1024 * per) return;
+        const int64_t piece = kNormThreads * kPartSlots * per;
+        const int64_t pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
+        parts = static_cast<int>((pieces + each - 1) / each);
+        length = static_cast<int>(each * piece);
+    }
+    size_t bytes() const { return up256(static_cast<size_t>(R) * static_cast<size_t>(parts) * sizeof(float4)); }
+};
+
 // Row groups of the backward pass: enough workgroups to fill the chip, eight rows to a group at least (its partial sums are
 // then a small part of what it reads).
 struct NormPlan {
@@ -210,13 +422,14 @@ bool misaligned(const void *p, int32_t dtype) { return reinterpret_cast<uintptr_
 
 extern "C" size_t rocket_layer_norm_workspace_bytes(int32_t rows, int32_t planes, int32_t n, int backward)
 {
-    if (rows < 1 || planes < 1 || n < 1 || !backward) return 0;
-    return NormPlan(rows, planes, n).bytes();
+    if (rows < 1 || planes < 1 || n < 1) return 0;
+    // the call's element type is not known here: fp32 rows take the most parts
+    return backward ? NormPlan(rows, planes, n).bytes() : ForwardPlan(rows, planes, n, ROCKET_F32).bytes();
 }
 
 extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows, int32_t planes, int32_t n, const float *weight_dev,
-                                 const float *bias_dev, float eps, void *y_dev, float *mean_dev, float *rstd_dev, void *, size_t,
-                                 void *hip_stream)
+                                 const float *bias_dev, float eps, void *y_dev, float *mean_dev, float *rstd_dev, void *ws,
+                                 size_t ws_bytes, void *hip_stream)
 {
     if (!x_dev || !y_dev) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: NULL pointer");
     if (!rk_type_known(dtype)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: unknown element type");
@@ -224,12 +437,38 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
     if (!std::isfinite(eps) || !(eps > 0.f)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: eps must be positive and finite");
     if (!mean_dev != !rstd_dev) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: mean and rstd go together");
     if (misaligned(x_dev, dtype) || misaligned(y_dev, dtype)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: x or y is not at an element's address");
-    const int64_t R = static_cast<int64_t>(rows) * planes;
+    const ForwardPlan plan(rows, planes, n, dtype);
+    if (plan.parts > 0 && (!ws || ws_bytes < plan.bytes() || reinterpret_cast<uintptr_t>(ws) % 16 != 0))
+        return rk_fail(ROCKET_EWORKSPACE, "rocket_layer_norm: an aligned workspace of " + std::to_string(plan.bytes()) + " bytes required");
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(rn_forward<T>, dim3(static_cast<unsigned>(std::min<int64_t>(R, 1 << 20))), dim3(kNormThreads), 0,
-                           static_cast<hipStream_t>(hip_stream), static_cast<const T *>(x_dev), R, planes, n, weight_dev, bias_dev, eps,
-                           static_cast<T *>(y_dev), mean_dev, rstd_dev);
+        const T *x = static_cast<const T *>(x_dev);
+        T *y = static_cast<T *>(y_dev);
+        const auto held = [&](auto lanes, auto slots) {
+            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, kRows = L < 256 ? 256 / L : 1;
+            hipLaunchKernelGGL((rn_forward<T, L, S>), dim3(static_cast<unsigned>((plan.R + kRows - 1) / kRows)), dim3(L < 256 ? 256 : L), 0, stream, x,
+                               plan.R, planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+        };
+        const int64_t loads = (n + kPerLoad<T> - 1) / kPerLoad<T>;      // of 16 bytes in a row
+        if (plan.parts == 0) {
+            if (loads <= 16) held(Int<16>(), Int<1>());
+            else if (loads <= 64) held(Int<64>(), Int<1>());
+            else if (loads <= 128) held(Int<64>(), Int<2>());
+            else if (loads <= 256) held(Int<64>(), Int<4>());
+            else if (loads <= 512) held(Int<64>(), Int<8>());
+            else if (loads <= 1024) held(Int<256>(), Int<4>());
+            else if (loads <= 2048) held(Int<256>(), Int<8>());
+            else if (loads <= 4096) held(Int<1024>(), Int<4>());
+            else held(Int<1024>(), Int<8>());
+        } else {
+            float4 *moments = static_cast<float4 *>(ws);
+            const unsigned tall = static_cast<unsigned>(std::min<int64_t>(plan.R, 32768));
+            hipLaunchKernelGGL(rn_forward_parts<T>, dim3(static_cast<unsigned>(plan.parts), tall), dim3(kNormThreads), 0, stream, x, plan.R, n, plan.length,
+                               moments);
+            hipLaunchKernelGGL(rn_forward_apply<T>, dim3(static_cast<unsigned>((n + int64_t{kPart<T>} - 1) / kPart<T>), tall), dim3(kNormThreads), 0, stream, x,
+                               plan.R, planes, n, plan.length, plan.parts, moments, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+        }
     });
     return hipGetLastError() == hipSuccess ? ROCKET_OK : rk_fail(ROCKET_EHIP, "launch of the layer norm kernel failed");
 }
