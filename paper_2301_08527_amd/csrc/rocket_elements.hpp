@@ -71,3 +71,21 @@ __device__ __forceinline__ void rk_load_f32(const float *p, int64_t left, float 
             if (i < left) v[i] = p[i];
     }
 }
+
+template <int N>
+__device__ __forceinline__ void rk_store_f32(float *p, int64_t left, const float (&v)[N])
+{
+    if (left >= N) {
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            RkSlot<float>::V q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = v[k + i];
+            reinterpret_cast<RkSlot<float> *>(p + k)->v = q;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) p[i] = v[i];
+    }
+}

@@ -266,109 +266,279 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int
     }
 }
 
-// Sums of N values over the workgroup, the same on every lane.
-template <int N, class S>
-__device__ __forceinline__ void rn_sum(S (&v)[N], S *lds)
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        for (int off = 32; off > 0; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
-    const int wave = static_cast<int>(threadIdx.x) >> 6;
-    __syncthreads();        // the last sums have been read
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) lds[wave * N + i] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        S s = 0;
-        for (int w = 0; w < kNormThreads / 64; ++w) s += lds[w * N + i];
-        v[i] = s;
-    }
-}
+// ------------------------------------------------------------------ backward
 
-// Row sums of the backward pass: {mean g, mean(g h), e, r} of every row.
-template <class T>
-__global__ __launch_bounds__(kNormThreads) void rn_backward_rows(const T *x, const T *dy, int64_t R, int planes, int n,
-                                                                 const float *__restrict__ weight, const float *__restrict__ mean,
-                                                                 const float *__restrict__ rstd, float4 *__restrict__ sums)
+// The partial sums of the weight's and the bias's gradient: one row of 2 * stride floats for each part of the rows, wide = planes * n
+// of each used.
+__device__ __host__ __forceinline__ int64_t rn_stride(int64_t wide) { return (wide + 3) / 4 * 4; }
+
+// A row of x and one of dy lie in the registers of LANES lanes as in the forward pass; the lanes go on to further rows of the same
+// plane and keep the sums of their columns, so x and dy are read once.  GROUPS rows at a time, whose sums meet in LDS at the end.
+// grid (parts of the rows, planes).  With one part the sums are the gradients.
+template <class T, int LANES, int SLOTS, int GROUPS>
+__global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const T *dy, int rows, int planes, int n, const float *__restrict__ weight,
+                                                              const float *__restrict__ mean, const float *__restrict__ rstd, T *dx,
+                                                              float *__restrict__ part, float *__restrict__ grad_w, float *__restrict__ grad_b)
 {
-    constexpr int N = kPerLoad<T>;
-    __shared__ double lds[3 * kNormThreads / 64];
-    for (int64_t row = blockIdx.x; row < R; row += gridDim.x) {
+    constexpr int N = kPerLoad<T>, kWaves = LANES > 64 ? LANES / 64 : 1, kWide = SLOTS * N * LANES;
+    static_assert(LANES <= 64 || GROUPS == 1, "a row of several wavefronts has the workgroup to itself");
+    __shared__ float meet[2][3][kWaves];
+    __shared__ float4 total[GROUPS > 1 ? 2 * kWide / 4 : 1];
+    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1), group = static_cast<int>(threadIdx.x) / LANES, i0 = lane * N, step = LANES * N;
+    const int plane = static_cast<int>(blockIdx.y), wave = static_cast<int>(threadIdx.x) >> 6;
+    const float per = 1.f / static_cast<float>(n);
+    constexpr bool kKeep = SLOTS < 5;       // the weights stay in registers, where there is room for them
+    float kept[kKeep ? SLOTS : 1][N], dw[SLOTS][N] = {}, db[SLOTS][N] = {};
+    const auto load_weights = [&](int i, float (&w)[N]) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) w[q] = 1.f;
+        if (weight && i < n) rk_load_f32<N>(weight + static_cast<int64_t>(plane) * n + i, n - i, w);
+    };
+    if constexpr (kKeep)
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) load_weights(i0 + k * step, kept[k]);
+    int turn = 0;
+    for (int64_t b = static_cast<int64_t>(blockIdx.x) * GROUPS + group; b < rows; b += static_cast<int64_t>(gridDim.x) * GROUPS, turn ^= 1) {
+        const int64_t row = b * planes + plane;
+        Held<T, SLOTS> xs, ds;
+        rn_hold<T, SLOTS>(xs, x + row * n, i0, step, n);
+        rn_hold<T, SLOTS>(ds, dy + row * n, i0, step, n);
         const float m = mean[row], r = rstd[row];
-        const int64_t w0 = row % planes * n;
-        float v[N], d[N];
-        double s[3] = {0.0, 0.0, 0.0};
-        for (int i = static_cast<int>(threadIdx.x) * N; i < n; i += kNormThreads * N) {
-            rk_load(x + row * n + i, n - i, v);
-            rk_load(dy + row * n + i, n - i, d);
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            const int left = n - (i0 + k * step);
+            if constexpr (!kKeep) load_weights(i0 + k * step, kept[0]);
+            const float (&w)[N] = kept[kKeep ? k : 0];
+#pragma unroll
             for (int q = 0; q < N; ++q) {
-                const float g = weight && i + q < n ? d[q] * weight[w0 + i + q] : d[q];
-                const float h = i + q < n ? (v[q] - m) * r : 0.f;
-                s[0] += static_cast<double>(g);
-                s[1] += static_cast<double>(g) * static_cast<double>(h);
-                s[2] += static_cast<double>(h);
+                const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
+                s[0] += g;
+                s[1] = fmaf(g, h, s[1]);
+                s[2] += q < left ? h : 0.f;
             }
         }
-        rn_sum(s, lds);
-        const double e = s[2] / n;
-        if (threadIdx.x == 0)
-            sums[row] = make_float4(static_cast<float>(s[0] / n), static_cast<float>((s[1] - e * s[0]) / n), static_cast<float>(e), r);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<LANES < 64 ? LANES : 64>(s[i]);
+        if constexpr (LANES > 64) {
+            // two sets of places by turns: one barrier to a row
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int i = 0; i < 3; ++i) meet[turn][i][wave] = s[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<16>(static_cast<int>(threadIdx.x & 15) < kWaves ? meet[turn][i][threadIdx.x & 15] : 0.f);
+        }
+        const float c1 = s[0] * per, e = s[2] * per, c2 = fmaf(-e, s[0], s[1]) * per;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            const int i = i0 + k * step;
+            if constexpr (!kKeep) load_weights(i, kept[0]);
+            const float (&w)[N] = kept[kKeep ? k : 0];
+            float v[N];
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const float h = fmaf(static_cast<float>(xs[k][q]) - m, r, -e), d = static_cast<float>(ds[k][q]);
+                dw[k][q] = fmaf(d, h, dw[k][q]);
+                db[k][q] += d;
+                v[q] = r * (fmaf(-h, c2, d * w[q]) - c1);
+            }
+            if (i < n) rk_store(dx + row * n + i, n - i, v);
+        }
+    }
+    if (!part && !grad_w && !grad_b) return;
+    if constexpr (GROUPS > 1) {
+        // the groups add their sums in turn, each lane's own four at a time
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            if (group == g) {
+#pragma unroll
+                for (int k = 0; k < SLOTS; ++k)
+#pragma unroll
+                    for (int q = 0; q < N; q += 4) {
+                        float4 &tw = total[((k * 2) * (N / 4) + q / 4) * LANES + lane], &tb = total[((k * 2 + 1) * (N / 4) + q / 4) * LANES + lane];
+                        float4 aw = make_float4(dw[k][q], dw[k][q + 1], dw[k][q + 2], dw[k][q + 3]);
+                        float4 ab = make_float4(db[k][q], db[k][q + 1], db[k][q + 2], db[k][q + 3]);
+                        if (g > 0) {
+                            const float4 ow = tw, ob = tb;
+                            aw = make_float4(ow.x + aw.x, ow.y + aw.y, ow.z + aw.z, ow.w + aw.w);
+                            ab = make_float4(ob.x + ab.x, ob.y + ab.y, ob.z + ab.z, ob.w + ab.w);
+                        }
+                        if (g < GROUPS - 1) {
+                            tw = aw;
+                            tb = ab;
+                        } else {
+                            dw[k][q] = aw.x; dw[k][q + 1] = aw.y; dw[k][q + 2] = aw.z; dw[k][q + 3] = aw.w;
+                            db[k][q] = ab.x; db[k][q + 1] = ab.y; db[k][q + 2] = ab.z; db[k][q + 3] = ab.w;
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+        if (group != GROUPS - 1) return;
+    }
+    const int64_t wide = static_cast<int64_t>(planes) * n, w0 = static_cast<int64_t>(plane) * n;
+    float *to_w = part ? part + 2 * rn_stride(wide) * blockIdx.x + w0 : grad_w ? grad_w + w0 : nullptr;
+    float *to_b = part ? part + 2 * rn_stride(wide) * blockIdx.x + rn_stride(wide) + w0 : grad_b ? grad_b + w0 : nullptr;
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+        const int i = i0 + k * step;
+        if (i >= n) break;
+        if (to_w) rk_store_f32<N>(to_w + i, n - i, dw[k]);
+        if (to_b) rk_store_f32<N>(to_b + i, n - i, db[k]);
     }
 }
 
-// A workgroup has kNormThreads * N columns of a plane and `per` of its rows: dx there, and the columns' partial sums of those rows.
-// grid (column tiles, planes, row groups)
+// Rows too long for that: sums {sum g, sum g h', sum h'} of parts of a row first.  Pieces of kPart values in fp32, joined in fp64.
+// grid (parts, R up to 2^15 and on)
 template <class T>
-__global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, const T *dy, int rows, int planes, int n, int per,
+__global__ __launch_bounds__(kNormThreads) void rn_backward_parts(const T *x, const T *dy, int64_t R, int planes, int n, int length,
+                                                                  const float *__restrict__ weight, const float *__restrict__ mean,
+                                                                  const float *__restrict__ rstd, float4 *__restrict__ sums)
+{
+    constexpr int N = kPerLoad<T>, kStep = kNormThreads * N;
+    __shared__ float meet[3][kNormThreads / 64];
+    for (int64_t row = blockIdx.y; row < R; row += gridDim.y) {
+        const float m = mean[row], r = rstd[row];
+        const int64_t w0 = row % planes * n;
+        const int64_t from = static_cast<int64_t>(blockIdx.x) * length, to = min(static_cast<int64_t>(n), from + length);
+        double total[3] = {0.0, 0.0, 0.0};
+        for (int64_t at = from; at < to; at += kPart<T>) {
+            const int some = static_cast<int>(min(to - at, static_cast<int64_t>(kPart<T>))), i0 = static_cast<int>(threadIdx.x) * N;
+            Held<T, kPartSlots> xs, ds;
+            rn_hold<T, kPartSlots>(xs, x + row * n + at, i0, kStep, some);
+            rn_hold<T, kPartSlots>(ds, dy + row * n + at, i0, kStep, some);
+            float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kPartSlots; ++k) {
+                const int i = i0 + k * kStep, left = some - i;
+                float w[N];
+#pragma unroll
+                for (int q = 0; q < N; ++q) w[q] = 1.f;
+                if (weight && left > 0) rk_load_f32<N>(weight + w0 + at + i, left, w);
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
+                    s[0] += g;
+                    s[1] = fmaf(g, h, s[1]);
+                    s[2] += q < left ? h : 0.f;
+                }
+            }
+            __syncthreads();        // the last piece's sums have been read
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                s[i] = rn_lanes_sum<64>(s[i]);
+                if ((threadIdx.x & 63) == 0) meet[i][threadIdx.x >> 6] = s[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+#pragma unroll
+                for (int v = 0; v < kNormThreads / 64; ++v) total[i] += static_cast<double>(meet[i][v]);
+        }
+        if (threadIdx.x == 0)
+            sums[row * gridDim.x + blockIdx.x] = make_float4(static_cast<float>(total[0]), static_cast<float>(total[1]), static_cast<float>(total[2]), 0.f);
+    }
+}
+
+// Then a workgroup has kNormThreads * N columns of a plane and `per` of its rows: dx there, and the columns' sums over those rows.
+// grid (column tiles, planes, parts of the rows), the last rows first: they were read last
+constexpr int kRowsAtOnce = kNormThreads / 4;
+template <class T>
+__global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, const T *dy, int rows, int planes, int n, int per, int parts,
                                                                     const float *__restrict__ weight, const float *__restrict__ mean,
-                                                                    const float4 *__restrict__ sums, T *dx, float *__restrict__ part)
+                                                                    const float *__restrict__ rstd, const float4 *__restrict__ sums, T *dx,
+                                                                    float *__restrict__ part)
 {
     constexpr int N = kPerLoad<T>;
-    const int plane = blockIdx.y, i = (static_cast<int>(blockIdx.x) * kNormThreads + static_cast<int>(threadIdx.x)) * N;
-    if (i >= n) return;
-    float wt[N], dw[N] = {}, db[N] = {}, v[N], d[N];
-    for (int q = 0; q < N; ++q) wt[q] = weight && i + q < n ? weight[static_cast<int64_t>(plane) * n + i + q] : 1.f;
-    const int from = static_cast<int>(blockIdx.z) * per, to = min(rows, from + per);
-    for (int b = from; b < to; ++b) {
-        const int64_t row = static_cast<int64_t>(b) * planes + plane;
-        const float4 s = sums[row];
-        const float m = mean[row];
-        rk_load(x + row * n + i, n - i, v);
-        rk_load(dy + row * n + i, n - i, d);
+    __shared__ float4 rs[kRowsAtOnce];      // m, r, e, c2
+    __shared__ float c1s[kRowsAtOnce];
+    const int plane = blockIdx.y, z = static_cast<int>(gridDim.z - 1 - blockIdx.z);
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * kNormThreads + static_cast<int>(threadIdx.x)) * N;
+    float w[N], dw[N] = {}, db[N] = {}, v[N], d[N];
 #pragma unroll
-        for (int q = 0; q < N; ++q) {
-            const float h = (v[q] - m) * s.w - s.z;
-            dw[q] = fmaf(d[q], h, dw[q]);
-            db[q] += d[q];
-            v[q] = s.w * (fmaf(-h, s.y, d[q] * wt[q]) - s.x);
+    for (int q = 0; q < N; ++q) w[q] = 1.f;
+    if (weight && i < n) rk_load_f32<N>(weight + static_cast<int64_t>(plane) * n + i, n - i, w);
+    const int from = z * per, to = static_cast<int>(min(static_cast<int64_t>(rows), static_cast<int64_t>(from) + per));
+    for (int at = from; at < to; at += kRowsAtOnce) {
+        const int some = min(to - at, kRowsAtOnce);
+        __syncthreads();        // the last rows are done with
+        {
+            // four lanes to a row add the sums of its parts
+            const int l = static_cast<int>(threadIdx.x) >> 2;
+            double s[3] = {0.0, 0.0, 0.0};
+            const int64_t row = (at + static_cast<int64_t>(min(l, some - 1))) * planes + plane;
+            for (int p = static_cast<int>(threadIdx.x) & 3; p < parts; p += 4) {
+                const float4 one = sums[row * parts + p];
+                s[0] += static_cast<double>(one.x);
+                s[1] += static_cast<double>(one.y);
+                s[2] += static_cast<double>(one.z);
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                s[k] += __shfl_xor(s[k], 1, 64);
+                s[k] += __shfl_xor(s[k], 2, 64);
+            }
+            if (l < some && (threadIdx.x & 3) == 0) {
+                const double e = s[2] / n;
+                rs[l] = make_float4(mean[row], rstd[row], static_cast<float>(e), static_cast<float>((s[1] - e * s[0]) / n));
+                c1s[l] = static_cast<float>(s[0] / n);
+            }
         }
-        rk_store(dx + row * n + i, n - i, v);
+        __syncthreads();
+        if (i >= n) continue;
+        for (int b = 0; b < some; ++b) {
+            const float4 c = rs[b];
+            const float c1 = c1s[b];
+            const int64_t place = ((at + static_cast<int64_t>(b)) * planes + plane) * n + i;
+            rk_load(x + place, n - i, v);
+            rk_load(dy + place, n - i, d);
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const float h = fmaf(v[q] - c.x, c.y, -c.z);
+                dw[q] = fmaf(d[q], h, dw[q]);
+                db[q] += d[q];
+                v[q] = c.y * (fmaf(-h, c.w, d[q] * w[q]) - c1);
+            }
+            rk_store(dx + place, n - i, v);
+        }
     }
-    const int64_t wide = static_cast<int64_t>(planes) * n;
-    float *to_w = part + 2 * static_cast<int64_t>(blockIdx.z) * wide + static_cast<int64_t>(plane) * n + i;
-    rk_store(to_w, n - i, *reinterpret_cast<float (*)[4]>(&dw[0]));
-    rk_store(to_w + wide, n - i, *reinterpret_cast<float (*)[4]>(&db[0]));
-    if constexpr (N == 8) {
-        rk_store(to_w + 4, n - i - 4, *reinterpret_cast<float (*)[4]>(&dw[4]));
-        rk_store(to_w + wide + 4, n - i - 4, *reinterpret_cast<float (*)[4]>(&db[4]));
-    }
+    if (!part || i >= n) return;
+    const int64_t stride = rn_stride(static_cast<int64_t>(planes) * n);
+    float *to_w = part + 2 * stride * z + static_cast<int64_t>(plane) * n + i;
+    rk_store_f32<N>(to_w, n - i, dw);
+    rk_store_f32<N>(to_w + stride, n - i, db);
 }
 
-// Sums of the row groups' partial sums, in their order.
-__global__ __launch_bounds__(kNormThreads) void rn_backward_finish(const float *__restrict__ part, int groups, int64_t wide,
-                                                                   float *__restrict__ dw, float *__restrict__ db)
+// The gradients from the parts' sums, in their order: COLUMNS columns to a workgroup, 4 a lane, the parts dealt out to the
+// kNormThreads / (COLUMNS / 4) lanes that a column then has; joined in fp64.
+template <int COLUMNS>
+__global__ __launch_bounds__(kNormThreads) void rn_backward_finish(const float *__restrict__ part, int parts, int64_t wide, float *__restrict__ dw,
+                                                                   float *__restrict__ db)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kNormThreads + threadIdx.x;
-    if (i >= wide) return;
-    double a = 0.0, b = 0.0;
-    for (int g = 0; g < groups; ++g) {
-        a += static_cast<double>(part[2 * g * wide + i]);
-        b += static_cast<double>(part[(2 * g + 1) * wide + i]);
+    constexpr int kAcross = COLUMNS / 4, kDown = kNormThreads / kAcross;
+    __shared__ double4 lds[kDown][kAcross];
+    const int64_t stride = rn_stride(wide), i = static_cast<int64_t>(blockIdx.x) * COLUMNS + (threadIdx.x % kAcross) * 4;
+    const int down = threadIdx.x / kAcross;
+    double4 s = {0.0, 0.0, 0.0, 0.0};
+    if (i < 2 * stride)
+#pragma unroll 4
+        for (int p = down; p < parts; p += kDown) {
+            const float4 v = *reinterpret_cast<const float4 *>(part + 2 * stride * p + i);
+            s.x += static_cast<double>(v.x); s.y += static_cast<double>(v.y); s.z += static_cast<double>(v.z); s.w += static_cast<double>(v.w);
+        }
+    lds[down][threadIdx.x % kAcross] = s;
+    __syncthreads();
+    if (threadIdx.x >= COLUMNS) return;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * COLUMNS + threadIdx.x;
+    double t = 0.0;
+#pragma unroll
+    for (int k = 0; k < kDown; ++k) t += reinterpret_cast<const double *>(&lds[k][threadIdx.x / 4])[threadIdx.x % 4];
+    if (at < wide) {
+        if (dw) dw[at] = static_cast<float>(t);
+    } else if (at >= stride && at < stride + wide) {
+        if (db) db[at - stride] = static_cast<float>(t);
     }
-    if (dw) dw[i] = static_cast<float>(a);
-    if (db) db[i] = static_cast<float>(b);
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -392,20 +562,44 @@ struct ForwardPlan {
     size_t bytes() const { return up256(static_cast<size_t>(R) * static_cast<size_t>(parts) * sizeof(float4)); }
 };
 
-// Row groups of the backward pass: enough workgroups to fill the chip, eight rows to a group at least (its partial sums are
-// then a small part of what it reads).
-struct NormPlan {
+// The backward pass.  `lanes` x `slots` hold a row (0: rows are too long and go in two passes); the rows of a plane are dealt out
+// to `parts` workgroups.
+struct BackwardPlan {
     int64_t R, wide;
-    int per, groups;
-    NormPlan(int32_t rows, int32_t planes, int32_t n) : R(static_cast<int64_t>(rows) * planes), wide(static_cast<int64_t>(planes) * n)
+    int lanes = 0, slots = 0, parts = 1;
+    int row_parts = 0, length = 0, per = 0;       // two passes: parts of a row, their length; rows of a part
+    BackwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes), wide(static_cast<int64_t>(planes) * n)
     {
-        const int64_t tiles = (n + kNormThreads * 4 - 1) / (kNormThreads * 4) * planes;
+        const int64_t per_load = 16 / static_cast<int64_t>(rk_type_bytes(dtype)), loads = (n + per_load - 1) / per_load;
+        const auto take = [&](int l, int s) { lanes = l, slots = s; };
+        if (loads <= 16) take(16, 1);
+        else if (loads <= 64) take(64, 1);
+        else if (loads <= 128) take(64, 2);
+        else if (loads <= 256) take(256, 1);
+        else if (loads <= 512) take(256, 2);
+        else if (loads <= 1024) take(512, 2);
+        else if (loads <= 2048) take(1024, 2);
+        else if (loads <= 4096 && dtype == ROCKET_F32) take(1024, 4);
+        else if (loads <= 5120 && dtype == ROCKET_F32) take(1024, 5);
+        if (lanes > 0) {
+            const int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
+            const int64_t turns = (static_cast<int64_t>(rows) + groups - 1) / groups;      // of all groups together
+            const int64_t most = std::max<int64_t>(1, 256 * 1024 / threads / planes);
+            parts = static_cast<int>(std::min(most, turns <= 16 ? 1 : turns));
+            if (parts > 1) parts = static_cast<int>((turns + (turns + parts - 1) / parts - 1) / ((turns + parts - 1) / parts));     // all take as many turns
+            return;
+        }
+        const int64_t piece = kNormThreads * kPartSlots * per_load, pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
+        row_parts = static_cast<int>((pieces + each - 1) / each);
+        length = static_cast<int>(each * piece);
+        const int64_t tiles = (n + kNormThreads * per_load - 1) / (kNormThreads * per_load) * planes;
         const int64_t want = std::min<int64_t>(std::max<int64_t>(1, 2048 / tiles), 4096);
         per = static_cast<int>(std::max<int64_t>(8, (rows + want - 1) / want));
-        groups = (rows + per - 1) / per;
+        parts = (rows + per - 1) / per;
     }
-    size_t sums_bytes() const { return up256(static_cast<size_t>(R) * sizeof(float4)); }
-    size_t bytes() const { return sums_bytes() + up256(static_cast<size_t>(2 * groups) * static_cast<size_t>(wide) * 4); }
+    size_t sums_bytes() const { return up256(static_cast<size_t>(R) * static_cast<size_t>(row_parts) * sizeof(float4)); }
+    size_t part_bytes() const { return row_parts == 0 && parts == 1 ? 0 : up256(static_cast<size_t>(2 * parts) * static_cast<size_t>(rn_stride(wide)) * 4); }
+    size_t bytes() const { return std::max<size_t>(256, sums_bytes() + part_bytes()); }
 };
 
 template <class F>
@@ -424,7 +618,8 @@ extern "C" size_t rocket_layer_norm_workspace_bytes(int32_t rows, int32_t planes
 {
     if (rows < 1 || planes < 1 || n < 1) return 0;
     // the call's element type is not known here: fp32 rows take the most parts
-    return backward ? NormPlan(rows, planes, n).bytes() : ForwardPlan(rows, planes, n, ROCKET_F32).bytes();
+    return backward ? std::max(BackwardPlan(rows, planes, n, ROCKET_F32).bytes(), BackwardPlan(rows, planes, n, ROCKET_BF16).bytes())
+                    : ForwardPlan(rows, planes, n, ROCKET_F32).bytes();
 }
 
 extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows, int32_t planes, int32_t n, const float *weight_dev,
@@ -483,23 +678,50 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
     if (misaligned(x_dev, dtype) || misaligned(grad_y_dev, dtype) || misaligned(grad_x_dev, dtype))
         return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: x, grad_y or grad_x is not at an element's address");
     if (planes > 65535) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: more than 65535 planes");
-    const NormPlan plan(rows, planes, n);
+    const BackwardPlan plan(rows, planes, n, dtype);
     if (!ws || ws_bytes < plan.bytes() || reinterpret_cast<uintptr_t>(ws) % 16 != 0)
         return rk_fail(ROCKET_EWORKSPACE, "rocket_layer_norm_backward: an aligned workspace of " + std::to_string(plan.bytes()) + " bytes required");
+    const bool sums_wanted = grad_weight_dev || grad_bias_dev;
     float4 *sums = static_cast<float4 *>(ws);
-    float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.sums_bytes());
+    float *part = sums_wanted && plan.part_bytes() > 0 ? reinterpret_cast<float *>(static_cast<char *>(ws) + plan.sums_bytes()) : nullptr;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     by_type(dtype, [&](auto t) {
         using T = decltype(t);
         const T *x = static_cast<const T *>(x_dev), *dy = static_cast<const T *>(grad_y_dev);
-        hipLaunchKernelGGL(rn_backward_rows<T>, dim3(static_cast<unsigned>(std::min<int64_t>(plan.R, 1 << 20))), dim3(kNormThreads), 0, stream, x, dy,
-                           plan.R, planes, n, weight_dev, mean_dev, rstd_dev, sums);
-        const unsigned tiles = static_cast<unsigned>((n + kNormThreads * kPerLoad<T> - 1) / (kNormThreads * kPerLoad<T>));
-        hipLaunchKernelGGL(rn_backward_columns<T>, dim3(tiles, static_cast<unsigned>(planes), static_cast<unsigned>(plan.groups)), dim3(kNormThreads), 0,
-                           stream, x, dy, rows, planes, n, plan.per, weight_dev, mean_dev, sums, static_cast<T *>(grad_x_dev), part);
-        if (grad_weight_dev || grad_bias_dev)
-            hipLaunchKernelGGL(rn_backward_finish, dim3(static_cast<unsigned>((plan.wide + kNormThreads - 1) / kNormThreads)), dim3(kNormThreads), 0, stream,
-                               part, plan.groups, plan.wide, grad_weight_dev, grad_bias_dev);
+        T *dx = static_cast<T *>(grad_x_dev);
+        const auto held = [&](auto lanes, auto slots) {
+            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, G = L < 256 ? 256 / L : 1;
+            if (plan.lanes != L || plan.slots != S) return;
+            hipLaunchKernelGGL((rn_backward<T, L, S, G>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)), dim3(L * G), 0, stream, x, dy,
+                               rows, planes, n, weight_dev, mean_dev, rstd_dev, dx, part, grad_weight_dev, grad_bias_dev);
+        };
+        held(Int<16>(), Int<1>());
+        held(Int<64>(), Int<1>());
+        held(Int<64>(), Int<2>());
+        held(Int<256>(), Int<1>());
+        held(Int<256>(), Int<2>());
+        held(Int<512>(), Int<2>());
+        held(Int<1024>(), Int<2>());
+        if constexpr (sizeof(T) == 4) {
+            held(Int<1024>(), Int<4>());
+            held(Int<1024>(), Int<5>());
+        }
+        if (plan.row_parts > 0) {
+            hipLaunchKernelGGL(rn_backward_parts<T>, dim3(static_cast<unsigned>(plan.row_parts), static_cast<unsigned>(std::min<int64_t>(plan.R, 32768))),
+                               dim3(kNormThreads), 0, stream, x, dy, plan.R, planes, n, plan.length, weight_dev, mean_dev, rstd_dev, sums);
+            const unsigned tiles = static_cast<unsigned>((n + int64_t{kNormThreads * kPerLoad<T>} - 1) / (kNormThreads * kPerLoad<T>));
+            hipLaunchKernelGGL(rn_backward_columns<T>, dim3(tiles, static_cast<unsigned>(planes), static_cast<unsigned>(plan.parts)), dim3(kNormThreads), 0,
+                               stream, x, dy, rows, planes, n, plan.per, plan.row_parts, weight_dev, mean_dev, rstd_dev, sums, dx, part);
+        }
+        if (part) {
+            const int64_t floats = 2 * rn_stride(plan.wide);
+            if (floats >= 64 * 512)
+                hipLaunchKernelGGL(rn_backward_finish<64>, dim3(static_cast<unsigned>((floats + 63) / 64)), dim3(kNormThreads), 0, stream, part, plan.parts,
+                                   plan.wide, grad_weight_dev, grad_bias_dev);
+            else
+                hipLaunchKernelGGL(rn_backward_finish<16>, dim3(static_cast<unsigned>((floats + 15) / 16)), dim3(kNormThreads), 0, stream, part, plan.parts,
+                                   plan.wide, grad_weight_dev, grad_bias_dev);
+        }
     });
     return hipGetLastError() == hipSuccess ? ROCKET_OK : rk_fail(ROCKET_EHIP, "launch of the layer norm's backward kernels failed");
 }
