@@ -355,7 +355,7 @@ int rocket_train_step(rocket_kernels *kernels, const void *x_dev, int x_is_u8, i
  * rocket_layer_norm: x_dev and y_dev (device, rows x planes x n of type dtype: ROCKET_F32, ROCKET_BF16 or ROCKET_F16; y_dev
  * may be x_dev), weight_dev and bias_dev (device, planes x n float32, either may be NULL: 1 and 0), mean_dev and rstd_dev
  * (device, rows x planes float32, both or neither NULL) receive m and r for the backward pass.  rows, planes, n >= 1,
- * eps > 0.
+ * planes <= 65535, n <= 2^30, eps > 0.  Squares of distances from the mean are fp32: values of a row lie within 1e18 of each other.
  *
  * rocket_layer_norm_backward: from grad_y_dev (type dtype) and the forward pass's x, mean and rstd, with g = grad_y weight
  * and h = (x - m) r

@@ -30,16 +30,17 @@ __device__ __forceinline__ float rn_dpp(float v)
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
 }
 
-// Sum over 16 or 64 neighbouring lanes, the same bits on each of them: rotations within the rows of 16 lanes, then the
-// rows' sums one after the other into the last row.
+// Sum over LANES neighbouring lanes, the same bits on each of them: within quads, then by reflections within eight and sixteen
+// lanes, then across the rows of sixteen.
 template <int LANES>
 __device__ __forceinline__ float rn_lanes_sum(float v)
 {
-    static_assert(LANES == 16 || LANES == 64, "a row of lanes or a wavefront");
-    v += rn_dpp<0x128, 0xf>(v);       // row_ror:8, 4, 2, 1
-    v += rn_dpp<0x124, 0xf>(v);
-    v += rn_dpp<0x122, 0xf>(v);
-    v += rn_dpp<0x121, 0xf>(v);
+    static_assert(LANES == 4 || LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "lanes that meet without LDS");
+    v += rn_dpp<0xB1, 0xf>(v);        // quad_perm 1,0,3,2 and 2,3,0,1
+    v += rn_dpp<0x4E, 0xf>(v);
+    if constexpr (LANES >= 8) v += rn_dpp<0x141, 0xf>(v);      // row_half_mirror
+    if constexpr (LANES >= 16) v += rn_dpp<0x140, 0xf>(v);     // row_mirror
+    if constexpr (LANES == 32) v += __shfl_xor(v, 16, 64);
     if constexpr (LANES == 64) {
         v += rn_dpp<0x142, 0xa>(v);   // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
         v += rn_dpp<0x143, 0xc>(v);
@@ -54,40 +55,99 @@ struct Moments {
     float count, shift, rest, m2;
 };
 
-// Of all values that the LANES lanes of a row hold in `raw`.  `left[s]` values of slot s exist, `n` of all lanes.
+// A row in the registers of its lanes, as it was loaded: slot k of LANES lanes together is values k * step .. (k + 1) * step - 1, and all
+// slots but the last are whole.  In the last one the lane that reaches over the end has the row's last N values instead, and so
+// have the lanes beyond it: no lane takes a way of its own (one that loads its values one by one keeps its wavefront waiting
+// for each).  Values that an earlier lane has too count in no sum; what is stored for them is the same bits twice.  Only rows
+// shorter than a slot (TINY) are loaded and stored value by value.
 template <class T, int SLOTS>
 using Held = typename RkSlot<T>::V[SLOTS];
 
 template <class T, int LANES, int SLOTS>
-__device__ __forceinline__ Moments rn_moments(const Held<T, SLOTS> &raw, int i0, int step, int n, float count)
+struct Place {
+    static constexpr int N = kPerLoad<T>, kStep = LANES * N;
+    static constexpr bool kTiny = LANES == 4;
+    int n, first, last, skip;      // values of the row; places of slots 0 and SLOTS - 1; values of the last one that do not count
+    bool tiny, some;               // some: the last slot has values that count
+    __device__ __forceinline__ Place(int n, int lane) : n(n)
+    {
+        const int i = lane * N + (SLOTS - 1) * kStep;
+        tiny = kTiny && n < N;
+        last = max(min(i, n - N), 0);
+        first = SLOTS > 1 ? lane * N : last;
+        skip = min(i - last, N);
+        some = tiny ? lane == 0 : skip < N;
+    }
+    __device__ __forceinline__ int at(int k) const { return k < SLOTS - 1 ? first + k * kStep : last; }
+    // whether value q of slot k counts
+    __device__ __forceinline__ bool counts(int k, int q) const { return k < SLOTS - 1 || (kTiny && tiny ? some && q < n : q >= skip); }
+};
+
+template <class T, int LANES, int SLOTS, bool STREAM>
+__device__ __forceinline__ void rn_hold(Held<T, SLOTS> &raw, const T *src, const Place<T, LANES, SLOTS> &place)
 {
     constexpr int N = kPerLoad<T>;
-    float s = 0.f;        // values that do not exist are zeros
+    if (place.kTiny && place.tiny) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) raw[0][q] = src[min(q, place.n - 1)];
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) raw[k] = rk_load_slot<T, STREAM>(src + place.at(k));
+}
+
+// N values of a plane's weights or biases beside those of slot k
+template <class T, int LANES, int SLOTS>
+__device__ __forceinline__ void rn_beside(const float *from, const Place<T, LANES, SLOTS> &place, int k, float (&v)[kPerLoad<T>])
+{
+    if (place.kTiny && place.tiny) {
+#pragma unroll
+        for (int q = 0; q < kPerLoad<T>; ++q) v[q] = from[min(q, place.n - 1)];
+        return;
+    }
+    rk_load_f32<kPerLoad<T>>(from + place.at(k), v);
+}
+
+template <class T, int LANES, int SLOTS, bool STREAM>
+__device__ __forceinline__ void rn_put(T *dst, const Place<T, LANES, SLOTS> &place, int k, const float (&v)[kPerLoad<T>])
+{
+    if (k == SLOTS - 1 && !place.some) return;
+    rk_store<T, STREAM>(dst + place.at(k), place.kTiny && place.tiny ? place.n : kPerLoad<T>, v);
+}
+
+// Keeps the compiler from carrying what it made of the slots (their values as floats, twice the registers of 16-bit ones) from one
+// pass over them to the next: made again, they cost an instruction or two.
+template <class T, int SLOTS>
+__device__ __forceinline__ void rn_forget(Held<T, SLOTS> &raw)
+{
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+        uint4 u = __builtin_bit_cast(uint4, raw[k]);
+        asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));
+        raw[k] = __builtin_bit_cast(typename RkSlot<T>::V, u);
+    }
+}
+
+// Moments of what LANES lanes hold of a row, `count` values; counts(k, q): whether value q of slot k does.
+template <class T, int LANES, int SLOTS, class F>
+__device__ __forceinline__ Moments rn_moments(const Held<T, SLOTS> &raw, float count, F counts)
+{
+    constexpr int N = kPerLoad<T>;
+    float s = 0.f;
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k)
 #pragma unroll
-        for (int q = 0; q < N; ++q) s += static_cast<float>(raw[k][q]);
+        for (int q = 0; q < N; ++q) s += counts(k, q) ? static_cast<float>(raw[k][q]) : 0.f;
     const float shift = rn_lanes_sum<LANES>(s) / count;
     float d1 = 0.f, d2 = 0.f;
 #pragma unroll
-    for (int k = 0; k < SLOTS; ++k) {
-        const int left = n - (i0 + k * step);
-        if (left >= N) {
+    for (int k = 0; k < SLOTS; ++k)
 #pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const float d = static_cast<float>(raw[k][q]) - shift;
-                d1 += d;
-                d2 = fmaf(d, d, d2);
-            }
-        } else if (left > 0) {
-#pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const float d = q < left ? static_cast<float>(raw[k][q]) - shift : 0.f;
-                d1 += d;
-                d2 = fmaf(d, d, d2);
-            }
+        for (int q = 0; q < N; ++q) {
+            const float d = counts(k, q) ? static_cast<float>(raw[k][q]) - shift : 0.f;
+            d1 += d;
+            d2 = fmaf(d, d, d2);
         }
-    }
     d1 = rn_lanes_sum<LANES>(d1);
     d2 = rn_lanes_sum<LANES>(d2);
     const float rest = d1 / count;
@@ -107,40 +167,11 @@ __device__ __forceinline__ Moments rn_join(const Moments &part, float n)
     return {n, shift, rest, rn_lanes_sum<16>(some ? fmaf(part.count * apart, apart, part.m2) : 0.f)};
 }
 
-template <class T, int SLOTS>
-__device__ __forceinline__ void rn_hold(Held<T, SLOTS> &raw, const T *src, int i0, int step, int n)
+template <int N>
+__device__ __forceinline__ void rn_normal(const float (&x)[N], const Moments &m, float r, const float (&w)[N], const float (&b)[N], float (&y)[N])
 {
-    constexpr int N = kPerLoad<T>;
 #pragma unroll
-    for (int k = 0; k < SLOTS; ++k) {
-        const int i = i0 + k * step;
-        if (i + N <= n) {
-            raw[k] = reinterpret_cast<const RkSlot<T> *>(src + i)->v;
-        } else {
-#pragma unroll
-            for (int q = 0; q < N; ++q) raw[k][q] = i + q < n ? src[i + q] : static_cast<T>(0.f);
-        }
-    }
-}
-
-template <class T, int SLOTS>
-__device__ __forceinline__ void rn_write(const Held<T, SLOTS> &raw, T *dst, int i0, int step, int n, const Moments &m, float r, const float *weight,
-                                         const float *bias)
-{
-    constexpr int N = kPerLoad<T>;
-#pragma unroll
-    for (int k = 0; k < SLOTS; ++k) {
-        const int i = i0 + k * step;
-        if (i >= n) break;
-        float v[N], w[N], b[N];
-#pragma unroll
-        for (int q = 0; q < N; ++q) w[q] = 1.f, b[q] = 0.f;
-        if (weight) rk_load_f32<N>(weight + i, n - i, w);
-        if (bias) rk_load_f32<N>(bias + i, n - i, b);
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = fmaf(((static_cast<float>(raw[k][q]) - m.shift) - m.rest) * r, w[q], b[q]);
-        rk_store(dst + i, n - i, v);
-    }
+    for (int q = 0; q < N; ++q) y[q] = fmaf(((x[q] - m.shift) - m.rest) * r, w[q], b[q]);
 }
 
 // n as a float: exact up to 2^24, and a rounding of 2^-25 of the mean of squares beyond
@@ -148,41 +179,68 @@ __device__ __forceinline__ float rn_rstd(const Moments &m, float eps) { return 1
 
 // A row lies in the registers of LANES lanes, SLOTS loads of 16 bytes in each (as loaded: 16-bit values take half the registers),
 // so x is read once.  Two passes over the registers give the mean and the distances from it; up to 64 lanes meet by lane
-// rotations alone, more lanes once through LDS, where the wavefronts' own means and sums of squares are joined.
-template <class T, int LANES, int SLOTS>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int64_t R, int planes, int n, const float *__restrict__ weight,
-                                                                        const float *__restrict__ bias, float eps, T *y,
-                                                                        float *__restrict__ mean, float *__restrict__ rstd)
+// exchanges alone, more lanes once through LDS, where the wavefronts' own means and sums of squares are joined.  Short rows: ROWS
+// of them to each group of lanes, loaded together.  Rows from `first` on.
+template <class T, int LANES, int SLOTS, int ROWS, bool STREAM>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int64_t first, int64_t R, int planes, int n,
+                                                                        const float *__restrict__ weight, const float *__restrict__ bias, float eps,
+                                                                        T *y, float *__restrict__ mean, float *__restrict__ rstd)
 {
-    constexpr int N = kPerLoad<T>, kRows = LANES < 256 ? 256 / LANES : 1;
-    __shared__ float4 lds[LANES > 64 ? 16 : 1];
-    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1), i0 = lane * N, step = LANES * N;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / LANES;
-    if (row >= R) return;
-    Held<T, SLOTS> raw;
-    rn_hold<T, SLOTS>(raw, x + row * n, i0, step, n);
-    Moments m;
-    if constexpr (LANES <= 64) {
-        m = rn_moments<T, LANES, SLOTS>(raw, i0, step, n, static_cast<float>(n));
-    } else {
-        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-        int count = 0;
+    constexpr int N = kPerLoad<T>, kGroups = LANES < 256 ? 256 / LANES : 1;
+    constexpr bool kEarly = ROWS == 1 && SLOTS * N <= 16;       // weights and biases are on their way while the lanes meet
+    static_assert(LANES <= 64 || (ROWS == 1 && LANES >= 256), "a row of several wavefronts has the workgroup to itself");
+    __shared__ float4 meet[LANES > 64 ? 16 : 1];
+    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1);
+    const int64_t row0 = first + static_cast<int64_t>(blockIdx.x) * (kGroups * ROWS) + threadIdx.x / LANES;
+    const Place<T, LANES, SLOTS> place(n, lane);
+    Held<T, SLOTS> raw[ROWS];
+    float w[kEarly ? SLOTS : 1][N], b[kEarly ? SLOTS : 1][N];
+    const auto load_beside = [&](int64_t w0, int k, float (&ww)[N], float (&bb)[N]) {
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k) count += min(max(n - (k * step + wave * 64 * N), 0), 64 * N);
-        const Moments own = rn_moments<T, 64, SLOTS>(raw, i0, step, n, static_cast<float>(max(count, 1)));
-        if (static_cast<int>(threadIdx.x) < 16) lds[threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[wave] = make_float4(static_cast<float>(count), own.shift, own.rest, own.m2);
-        __syncthreads();
-        const float4 part = lds[threadIdx.x & 15];
-        m = rn_join({part.x, part.y, part.z, part.w}, static_cast<float>(n));
-    }
-    const float r = rn_rstd(m, eps);
-    const int64_t w0 = row % planes * n;
-    rn_write<T, SLOTS>(raw, y + row * n, i0, step, n, m, r, weight ? weight + w0 : nullptr, bias ? bias + w0 : nullptr);
-    if (mean && lane == 0) {
-        mean[row] = m.shift + m.rest;
-        rstd[row] = r;
+        for (int q = 0; q < N; ++q) ww[q] = 1.f, bb[q] = 0.f;
+        if (weight) rn_beside(weight + w0, place, k, ww);
+        if (bias) rn_beside(bias + w0, place, k, bb);
+    };
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j)      // rows beyond the last: the last once more
+        rn_hold<T, LANES, SLOTS, STREAM>(raw[j], x + min(row0 + j * kGroups, R - 1) * n, place);
+    if constexpr (kEarly)
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) load_beside(min(row0, R - 1) % planes * n, k, w[k], b[k]);
+    const auto counts = [&](int k, int q) { return place.counts(k, q); };
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        const int64_t row = row0 + j * kGroups;
+        Moments m;
+        if constexpr (LANES <= 64) {
+            m = rn_moments<T, LANES, SLOTS>(raw[j], static_cast<float>(n), counts);
+        } else {
+            const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+            const int count = (SLOTS - 1) * 64 * N + min(max(n - ((SLOTS - 1) * place.kStep + wave * 64 * N), 0), 64 * N);
+            const Moments own = rn_moments<T, 64, SLOTS>(raw[j], static_cast<float>(max(count, 1)), counts);
+            if ((threadIdx.x & 63) == 0) meet[wave] = make_float4(static_cast<float>(count), own.shift, own.rest, own.m2);
+            if (static_cast<int>(threadIdx.x) >= LANES - 64 && static_cast<int>(threadIdx.x & 63) > 0 && wave + static_cast<int>(threadIdx.x & 63) < 16)
+                meet[wave + (threadIdx.x & 63)] = make_float4(0.f, 0.f, 0.f, 0.f);        // places that no wavefront has
+            __syncthreads();
+            const float4 part = meet[threadIdx.x & 15];
+            m = rn_join({part.x, part.y, part.z, part.w}, static_cast<float>(n));
+        }
+        if (row >= R) continue;
+        if constexpr (sizeof(T) == 2) rn_forget<T, SLOTS>(raw[j]);
+        const float r = rn_rstd(m, eps);
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            float v[N], out[N];
+            if constexpr (!kEarly) load_beside(row % planes * n, k, w[0], b[0]);
+#pragma unroll
+            for (int q = 0; q < N; ++q) v[q] = static_cast<float>(raw[j][k][q]);
+            rn_normal(v, m, r, w[kEarly ? k : 0], b[kEarly ? k : 0], out);
+            rn_put<T, LANES, SLOTS, STREAM>(y + row * n, place, k, out);
+        }
+        if (mean && lane == 0) {
+            mean[row] = m.shift + m.rest;
+            rstd[row] = r;
+        }
     }
 }
 
@@ -192,6 +250,26 @@ constexpr int kMostParts = 64, kPartSlots = 4;
 template <class T>
 constexpr int kPart = kNormThreads * kPartSlots * kPerLoad<T>;
 
+// The slots of a piece from value `from` of a row of n on; whole: the row has all of them (else zeros beyond its end)
+template <class T, class F>
+__device__ __forceinline__ void rn_piece(Held<T, kPartSlots> &raw, const T *src, int from, int n, F whole)
+{
+    constexpr int N = kPerLoad<T>;
+#pragma unroll
+    for (int k = 0; k < kPartSlots; ++k) {
+        const int i = from + (k * kNormThreads + static_cast<int>(threadIdx.x)) * N;
+        raw[k] = whole ? rk_load_slot<T, false>(src + i) : rk_load_edge<T, false, false>(src, i, n);
+    }
+}
+
+// f(true_type) or f(false_type): one copy of the code for whole pieces, one for the last
+template <class F>
+__device__ __forceinline__ void rn_by_whole(bool whole, F f)
+{
+    if (whole) f(std::true_type());
+    else f(std::false_type());
+}
+
 template <class T>
 __global__ __launch_bounds__(kNormThreads) void rn_forward_parts(const T *x, int64_t R, int n, int length, float4 *__restrict__ moments)
 {
@@ -199,16 +277,21 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_parts(const T *x, int
     __shared__ float4 lds[16];
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     for (int64_t row = blockIdx.y; row < R; row += gridDim.y) {
-        const int from = static_cast<int>(blockIdx.x) * length, to = min(n - from, length) + from;
+        const int from = static_cast<int>(blockIdx.x) * length, to = from + min(n - from, length);
         Moments m = {0.f, 0.f, 0.f, 0.f};
-        for (int64_t at = from; at < to; at += kPart<T>) {
-            const int some = static_cast<int>(min(static_cast<int64_t>(to) - at, static_cast<int64_t>(kPart<T>)));
-            Held<T, kPartSlots> raw;
-            rn_hold<T, kPartSlots>(raw, x + row * n + at, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some);
+        for (int at = from; at < to; at += kPart<T>) {
+            const int some = min(to - at, kPart<T>);
             int count = 0;
+            Moments own;
+            rn_by_whole(some == kPart<T>, [&](auto whole) {
+                Held<T, kPartSlots> raw;
+                rn_piece<T>(raw, x + row * n, at, n, whole);
 #pragma unroll
-            for (int k = 0; k < kPartSlots; ++k) count += min(max(some - (k * kNormThreads * N + wave * 64 * N), 0), 64 * N);
-            const Moments own = rn_moments<T, 64, kPartSlots>(raw, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some, static_cast<float>(max(count, 1)));
+                for (int k = 0; k < kPartSlots; ++k) count += whole ? 64 * N : min(max(some - (k * kNormThreads * N + wave * 64 * N), 0), 64 * N);
+                own = rn_moments<T, 64, kPartSlots>(raw, static_cast<float>(max(count, 1)), [&](int k, int q) {
+                    return whole || (k * kNormThreads + static_cast<int>(threadIdx.x)) * N + q < some;
+                });
+            });
             __syncthreads();      // the last piece has been read
             if (static_cast<int>(threadIdx.x) < 16) lds[threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
             __syncthreads();
@@ -253,12 +336,28 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int
         const Moments m = rn_row_moments(moments + row * parts, parts);
         const float r = rn_rstd(m, eps);
         const int64_t w0 = row % planes * n;
-        const int64_t from = static_cast<int64_t>(blockIdx.x) * kPart<T>;
-        const int some = static_cast<int>(min(static_cast<int64_t>(n) - from, static_cast<int64_t>(kPart<T>)));
-        Held<T, kPartSlots> raw;
-        rn_hold<T, kPartSlots>(raw, x + row * n + from, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some);
-        rn_write<T, kPartSlots>(raw, y + row * n + from, static_cast<int>(threadIdx.x) * N, kNormThreads * N, some, m, r,
-                                weight ? weight + w0 + from : nullptr, bias ? bias + w0 + from : nullptr);
+        const int from = static_cast<int>(blockIdx.x) * kPart<T>;
+        rn_by_whole(from + kPart<T> <= n, [&](auto whole) {
+            Held<T, kPartSlots> raw;
+            rn_piece<T>(raw, x + row * n, from, n, whole);
+#pragma unroll
+            for (int k = 0; k < kPartSlots; ++k) {
+                const int i = from + (k * kNormThreads + static_cast<int>(threadIdx.x)) * N;
+                float v[N], w[N], b[N], out[N];
+#pragma unroll
+                for (int q = 0; q < N; ++q) v[q] = static_cast<float>(raw[k][q]), w[q] = 1.f, b[q] = 0.f;
+                if (weight) {
+                    if constexpr (whole) rk_load_f32<N>(weight + w0 + i, w);
+                    else rk_load_f32_edge<N, false>(weight + w0, i, n, w);
+                }
+                if (bias) {
+                    if constexpr (whole) rk_load_f32<N>(bias + w0 + i, b);
+                    else rk_load_f32_edge<N, false>(bias + w0, i, n, b);
+                }
+                rn_normal(v, m, r, w, b, out);
+                if (whole || i < n) rk_store<T, false>(y + row * n + i, whole ? N : n - i, out);
+            }
+        });
         if (mean && blockIdx.x == 0 && threadIdx.x == 0) {
             mean[row] = m.shift + m.rest;
             rstd[row] = r;
@@ -275,7 +374,7 @@ __device__ __host__ __forceinline__ int64_t rn_stride(int64_t wide) { return (wi
 // A row of x and one of dy lie in the registers of LANES lanes as in the forward pass; the lanes go on to further rows of the same
 // plane and keep the sums of their columns, so x and dy are read once.  GROUPS rows at a time, whose sums meet in LDS at the end.
 // grid (parts of the rows, planes).  With one part the sums are the gradients.
-template <class T, int LANES, int SLOTS, int GROUPS>
+template <class T, int LANES, int SLOTS, int GROUPS, bool STREAM>
 __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const T *dy, int rows, int planes, int n, const float *__restrict__ weight,
                                                               const float *__restrict__ mean, const float *__restrict__ rstd, T *dx,
                                                               float *__restrict__ part, float *__restrict__ grad_w, float *__restrict__ grad_b)
@@ -284,42 +383,46 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
     static_assert(LANES <= 64 || GROUPS == 1, "a row of several wavefronts has the workgroup to itself");
     __shared__ float meet[2][3][kWaves];
     __shared__ float4 total[GROUPS > 1 ? 2 * kWide / 4 : 1];
-    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1), group = static_cast<int>(threadIdx.x) / LANES, i0 = lane * N, step = LANES * N;
+    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1), group = static_cast<int>(threadIdx.x) / LANES;
     const int plane = static_cast<int>(blockIdx.y), wave = static_cast<int>(threadIdx.x) >> 6;
+    const int64_t w0 = static_cast<int64_t>(plane) * n;
+    const Place<T, LANES, SLOTS> place(n, lane);
     const float per = 1.f / static_cast<float>(n);
-    constexpr bool kKeep = SLOTS < 5;       // the weights stay in registers, where there is room for them
+    constexpr bool kKeep = SLOTS * N <= 16 && SLOTS < 4;       // the weights stay in registers, where there is room for them
     float kept[kKeep ? SLOTS : 1][N], dw[SLOTS][N] = {}, db[SLOTS][N] = {};
-    const auto load_weights = [&](int i, float (&w)[N]) {
+    const auto load_weights = [&](const float *from, int k, float (&w)[N]) {
 #pragma unroll
         for (int q = 0; q < N; ++q) w[q] = 1.f;
-        if (weight && i < n) rk_load_f32<N>(weight + static_cast<int64_t>(plane) * n + i, n - i, w);
+        if (from) rn_beside(from + w0, place, k, w);
     };
     if constexpr (kKeep)
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k) load_weights(i0 + k * step, kept[k]);
+        for (int k = 0; k < SLOTS; ++k) load_weights(weight, k, kept[k]);
     int turn = 0;
     for (int64_t b = static_cast<int64_t>(blockIdx.x) * GROUPS + group; b < rows; b += static_cast<int64_t>(gridDim.x) * GROUPS, turn ^= 1) {
         const int64_t row = b * planes + plane;
         Held<T, SLOTS> xs, ds;
-        rn_hold<T, SLOTS>(xs, x + row * n, i0, step, n);
-        rn_hold<T, SLOTS>(ds, dy + row * n, i0, step, n);
+        rn_hold<T, LANES, SLOTS, STREAM>(xs, x + row * n, place);
+        rn_hold<T, LANES, SLOTS, STREAM>(ds, dy + row * n, place);
         const float m = mean[row], r = rstd[row];
+        const float *again = weight;
+        if constexpr (!kKeep) asm volatile("" : "+s"(again));       // or the loads are moved out of the loop, into registers that are not there
         float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
-            const int left = n - (i0 + k * step);
-            if constexpr (!kKeep) load_weights(i0 + k * step, kept[0]);
+            if constexpr (!kKeep) load_weights(again, k, kept[0]);
             const float (&w)[N] = kept[kKeep ? k : 0];
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
-                s[0] += g;
-                s[1] = fmaf(g, h, s[1]);
-                s[2] += q < left ? h : 0.f;
+                const bool count = place.counts(k, q);
+                s[0] += count ? g : 0.f;
+                s[1] += count ? g * h : 0.f;
+                s[2] += count ? h : 0.f;
             }
         }
 #pragma unroll
-        for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<LANES < 64 ? LANES : 64>(s[i]);
+        for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<(LANES < 64 ? LANES : 64)>(s[i]);
         if constexpr (LANES > 64) {
             // two sets of places by turns: one barrier to a row
             if ((threadIdx.x & 63) == 0)
@@ -330,10 +433,11 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
             for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<16>(static_cast<int>(threadIdx.x & 15) < kWaves ? meet[turn][i][threadIdx.x & 15] : 0.f);
         }
         const float c1 = s[0] * per, e = s[2] * per, c2 = fmaf(-e, s[0], s[1]) * per;
+        rn_forget<T, SLOTS>(xs);
+        rn_forget<T, SLOTS>(ds);
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
-            const int i = i0 + k * step;
-            if constexpr (!kKeep) load_weights(i, kept[0]);
+            if constexpr (!kKeep) load_weights(again, k, kept[0]);
             const float (&w)[N] = kept[kKeep ? k : 0];
             float v[N];
 #pragma unroll
@@ -343,7 +447,7 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
                 db[k][q] += d;
                 v[q] = r * (fmaf(-h, c2, d * w[q]) - c1);
             }
-            if (i < n) rk_store(dx + row * n + i, n - i, v);
+            rn_put<T, LANES, SLOTS, STREAM>(dx + row * n, place, k, v);
         }
     }
     if (!part && !grad_w && !grad_b) return;
@@ -377,15 +481,15 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
         }
         if (group != GROUPS - 1) return;
     }
-    const int64_t wide = static_cast<int64_t>(planes) * n, w0 = static_cast<int64_t>(plane) * n;
-    float *to_w = part ? part + 2 * rn_stride(wide) * blockIdx.x + w0 : grad_w ? grad_w + w0 : nullptr;
-    float *to_b = part ? part + 2 * rn_stride(wide) * blockIdx.x + rn_stride(wide) + w0 : grad_b ? grad_b + w0 : nullptr;
+    const int64_t stride = rn_stride(static_cast<int64_t>(planes) * n);
+    float *to_w = part ? part + 2 * stride * blockIdx.x + w0 : grad_w ? grad_w + w0 : nullptr;
+    float *to_b = part ? part + 2 * stride * blockIdx.x + stride + w0 : grad_b ? grad_b + w0 : nullptr;
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k) {
-        const int i = i0 + k * step;
-        if (i >= n) break;
-        if (to_w) rk_store_f32<N>(to_w + i, n - i, dw[k]);
-        if (to_b) rk_store_f32<N>(to_b + i, n - i, db[k]);
+        if (k == SLOTS - 1 && !place.some) break;
+        const int left = place.kTiny && place.tiny ? n : N;
+        if (to_w) rk_store_f32<N>(to_w + place.at(k), left, dw[k]);
+        if (to_b) rk_store_f32<N>(to_b + place.at(k), left, db[k]);
     }
 }
 
@@ -396,34 +500,38 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_parts(const T *x, co
                                                                   const float *__restrict__ weight, const float *__restrict__ mean,
                                                                   const float *__restrict__ rstd, float4 *__restrict__ sums)
 {
-    constexpr int N = kPerLoad<T>, kStep = kNormThreads * N;
+    constexpr int N = kPerLoad<T>;
     __shared__ float meet[3][kNormThreads / 64];
     for (int64_t row = blockIdx.y; row < R; row += gridDim.y) {
         const float m = mean[row], r = rstd[row];
         const int64_t w0 = row % planes * n;
-        const int64_t from = static_cast<int64_t>(blockIdx.x) * length, to = min(static_cast<int64_t>(n), from + length);
+        const int from = static_cast<int>(blockIdx.x) * length, to = from + min(n - from, length);
         double total[3] = {0.0, 0.0, 0.0};
-        for (int64_t at = from; at < to; at += kPart<T>) {
-            const int some = static_cast<int>(min(to - at, static_cast<int64_t>(kPart<T>))), i0 = static_cast<int>(threadIdx.x) * N;
-            Held<T, kPartSlots> xs, ds;
-            rn_hold<T, kPartSlots>(xs, x + row * n + at, i0, kStep, some);
-            rn_hold<T, kPartSlots>(ds, dy + row * n + at, i0, kStep, some);
+        for (int at = from; at < to; at += kPart<T>) {
             float s[3] = {0.f, 0.f, 0.f};
+            rn_by_whole(at + kPart<T> <= n, [&](auto whole) {
+                Held<T, kPartSlots> xs, ds;
+                rn_piece<T>(xs, x + row * n, at, n, whole);
+                rn_piece<T>(ds, dy + row * n, at, n, whole);
 #pragma unroll
-            for (int k = 0; k < kPartSlots; ++k) {
-                const int i = i0 + k * kStep, left = some - i;
-                float w[N];
+                for (int k = 0; k < kPartSlots; ++k) {
+                    const int i = at + (k * kNormThreads + static_cast<int>(threadIdx.x)) * N;
+                    float w[N];
 #pragma unroll
-                for (int q = 0; q < N; ++q) w[q] = 1.f;
-                if (weight && left > 0) rk_load_f32<N>(weight + w0 + at + i, left, w);
+                    for (int q = 0; q < N; ++q) w[q] = 1.f;
+                    if (weight) {
+                        if constexpr (whole) rk_load_f32<N>(weight + w0 + i, w);
+                        else rk_load_f32_edge<N, false>(weight + w0, i, n, w);
+                    }
 #pragma unroll
-                for (int q = 0; q < N; ++q) {
-                    const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
-                    s[0] += g;
-                    s[1] = fmaf(g, h, s[1]);
-                    s[2] += q < left ? h : 0.f;
+                    for (int q = 0; q < N; ++q) {
+                        const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
+                        s[0] += g;
+                        s[1] = fmaf(g, h, s[1]);
+                        s[2] += whole || i + q < n ? h : 0.f;
+                    }
                 }
-            }
+            });
             __syncthreads();        // the last piece's sums have been read
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
@@ -454,11 +562,12 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, 
     __shared__ float4 rs[kRowsAtOnce];      // m, r, e, c2
     __shared__ float c1s[kRowsAtOnce];
     const int plane = blockIdx.y, z = static_cast<int>(gridDim.z - 1 - blockIdx.z);
-    const int64_t i = (static_cast<int64_t>(blockIdx.x) * kNormThreads + static_cast<int>(threadIdx.x)) * N;
-    float w[N], dw[N] = {}, db[N] = {}, v[N], d[N];
+    const int i = (static_cast<int>(blockIdx.x) * kNormThreads + static_cast<int>(threadIdx.x)) * N;
+    const bool all = static_cast<int>(blockIdx.x + 1) * (kNormThreads * N) <= n;      // columns of the workgroup exist
+    float w[N], dw[N] = {}, db[N] = {}, v[N];
 #pragma unroll
     for (int q = 0; q < N; ++q) w[q] = 1.f;
-    if (weight && i < n) rk_load_f32<N>(weight + static_cast<int64_t>(plane) * n + i, n - i, w);
+    if (weight) rk_load_f32_edge<N, false>(weight + static_cast<int64_t>(plane) * n, i, n, w);
     const int from = z * per, to = static_cast<int>(min(static_cast<int64_t>(rows), static_cast<int64_t>(from) + per));
     for (int at = from; at < to; at += kRowsAtOnce) {
         const int some = min(to - at, kRowsAtOnce);
@@ -486,22 +595,23 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, 
             }
         }
         __syncthreads();
-        if (i >= n) continue;
-        for (int b = 0; b < some; ++b) {
-            const float4 c = rs[b];
-            const float c1 = c1s[b];
-            const int64_t place = ((at + static_cast<int64_t>(b)) * planes + plane) * n + i;
-            rk_load(x + place, n - i, v);
-            rk_load(dy + place, n - i, d);
+        rn_by_whole(all, [&](auto whole) {
+            for (int b = 0; b < some; ++b) {
+                const float4 c = rs[b];
+                const float c1 = c1s[b];
+                const int64_t place = ((at + static_cast<int64_t>(b)) * planes + plane) * n;
+                const auto xs = whole ? rk_load_slot<T, false>(x + place + i) : rk_load_edge<T, false, false>(x + place, i, n);
+                const auto ds = whole ? rk_load_slot<T, false>(dy + place + i) : rk_load_edge<T, false, false>(dy + place, i, n);
 #pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const float h = fmaf(v[q] - c.x, c.y, -c.z);
-                dw[q] = fmaf(d[q], h, dw[q]);
-                db[q] += d[q];
-                v[q] = c.y * (fmaf(-h, c.w, d[q] * w[q]) - c1);
+                for (int q = 0; q < N; ++q) {
+                    const float h = fmaf(static_cast<float>(xs[q]) - c.x, c.y, -c.z), d = static_cast<float>(ds[q]);
+                    dw[q] = fmaf(d, h, dw[q]);
+                    db[q] += d;
+                    v[q] = c.y * (fmaf(-h, c.w, d * w[q]) - c1);
+                }
+                if (whole || i < n) rk_store<T, false>(dx + place + i, whole ? N : n - i, v);
             }
-            rk_store(dx + place, n - i, v);
-        }
+        });
     }
     if (!part || i >= n) return;
     const int64_t stride = rn_stride(static_cast<int64_t>(planes) * n);
@@ -518,30 +628,38 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_finish(const float *
 {
     constexpr int kAcross = COLUMNS / 4, kDown = kNormThreads / kAcross;
     __shared__ double4 lds[kDown][kAcross];
-    const int64_t stride = rn_stride(wide), i = static_cast<int64_t>(blockIdx.x) * COLUMNS + (threadIdx.x % kAcross) * 4;
+    const int64_t stride = rn_stride(wide);
     const int down = threadIdx.x / kAcross;
-    double4 s = {0.0, 0.0, 0.0, 0.0};
-    if (i < 2 * stride)
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * COLUMNS; first < 2 * stride; first += static_cast<int64_t>(gridDim.x) * COLUMNS) {
+        const int64_t i = first + (threadIdx.x % kAcross) * 4;
+        double4 s = {0.0, 0.0, 0.0, 0.0};
+        if (i < 2 * stride)
 #pragma unroll 4
-        for (int p = down; p < parts; p += kDown) {
-            const float4 v = *reinterpret_cast<const float4 *>(part + 2 * stride * p + i);
-            s.x += static_cast<double>(v.x); s.y += static_cast<double>(v.y); s.z += static_cast<double>(v.z); s.w += static_cast<double>(v.w);
-        }
-    lds[down][threadIdx.x % kAcross] = s;
-    __syncthreads();
-    if (threadIdx.x >= COLUMNS) return;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * COLUMNS + threadIdx.x;
-    double t = 0.0;
+            for (int p = down; p < parts; p += kDown) {
+                const float4 v = *reinterpret_cast<const float4 *>(part + 2 * stride * p + i);
+                s.x += static_cast<double>(v.x); s.y += static_cast<double>(v.y); s.z += static_cast<double>(v.z); s.w += static_cast<double>(v.w);
+            }
+        __syncthreads();        // the last columns have been read
+        lds[down][threadIdx.x % kAcross] = s;
+        __syncthreads();
+        if (threadIdx.x >= COLUMNS) continue;
+        const int64_t at = first + threadIdx.x;
+        double t = 0.0;
 #pragma unroll
-    for (int k = 0; k < kDown; ++k) t += reinterpret_cast<const double *>(&lds[k][threadIdx.x / 4])[threadIdx.x % 4];
-    if (at < wide) {
-        if (dw) dw[at] = static_cast<float>(t);
-    } else if (at >= stride && at < stride + wide) {
-        if (db) db[at - stride] = static_cast<float>(t);
+        for (int k = 0; k < kDown; ++k) t += reinterpret_cast<const double *>(&lds[k][threadIdx.x / 4])[threadIdx.x % 4];
+        if (at < wide) {
+            if (dw) dw[at] = static_cast<float>(t);
+        } else if (at >= stride && at < stride + wide) {
+            if (db) db[at - stride] = static_cast<float>(t);
+        }
     }
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+constexpr int32_t kMostPlanes = 65535;        // a launch's second dimension
+constexpr int32_t kMostValues = 1 << 30;      // of a row: its slots' numbers stay within 32 bits
+constexpr int64_t kMostGroups = 1 << 20;      // of a launch (its lanes must be fewer than 2^32)
 
 template <int V>
 using Int = std::integral_constant<int, V>;
@@ -572,15 +690,17 @@ struct BackwardPlan {
     {
         const int64_t per_load = 16 / static_cast<int64_t>(rk_type_bytes(dtype)), loads = (n + per_load - 1) / per_load;
         const auto take = [&](int l, int s) { lanes = l, slots = s; };
-        if (loads <= 16) take(16, 1);
+        if (loads <= 4) take(4, 1);
+        else if (loads <= 8) take(8, 1);
+        else if (loads <= 16) take(16, 1);
+        else if (loads <= 32) take(32, 1);
         else if (loads <= 64) take(64, 1);
         else if (loads <= 128) take(64, 2);
         else if (loads <= 256) take(256, 1);
-        else if (loads <= 512) take(256, 2);
-        else if (loads <= 1024) take(512, 2);
+        else if (loads <= 512) take(512, 1);
+        else if (loads <= 1024) take(1024, 1);
         else if (loads <= 2048) take(1024, 2);
-        else if (loads <= 4096 && dtype == ROCKET_F32) take(1024, 4);
-        else if (loads <= 5120 && dtype == ROCKET_F32) take(1024, 5);
+        else if (loads <= 5 * 1024 && dtype == ROCKET_F32) take(1024, static_cast<int>((loads + 1023) / 1024));
         if (lanes > 0) {
             const int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
             const int64_t turns = (static_cast<int64_t>(rows) + groups - 1) / groups;      // of all groups together
@@ -616,7 +736,7 @@ bool misaligned(const void *p, int32_t dtype) { return reinterpret_cast<uintptr_
 
 extern "C" size_t rocket_layer_norm_workspace_bytes(int32_t rows, int32_t planes, int32_t n, int backward)
 {
-    if (rows < 1 || planes < 1 || n < 1) return 0;
+    if (rows < 1 || planes < 1 || n < 1 || planes > kMostPlanes || n > kMostValues) return 0;
     // the call's element type is not known here: fp32 rows take the most parts
     return backward ? std::max(BackwardPlan(rows, planes, n, ROCKET_F32).bytes(), BackwardPlan(rows, planes, n, ROCKET_BF16).bytes())
                     : ForwardPlan(rows, planes, n, ROCKET_F32).bytes();
@@ -628,7 +748,8 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
 {
     if (!x_dev || !y_dev) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: NULL pointer");
     if (!rk_type_known(dtype)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: unknown element type");
-    if (rows < 1 || planes < 1 || n < 1) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: rows, planes and n must be >= 1");
+    if (rows < 1 || planes < 1 || n < 1 || planes > kMostPlanes || n > kMostValues)
+        return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: rows, planes and n must be >= 1, planes <= 65535, n <= 2^30");
     if (!std::isfinite(eps) || !(eps > 0.f)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: eps must be positive and finite");
     if (!mean_dev != !rstd_dev) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: mean and rstd go together");
     if (misaligned(x_dev, dtype) || misaligned(y_dev, dtype)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm: x or y is not at an element's address");
@@ -640,22 +761,34 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
         using T = decltype(t);
         const T *x = static_cast<const T *>(x_dev);
         T *y = static_cast<T *>(y_dev);
-        const auto held = [&](auto lanes, auto slots) {
-            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, kRows = L < 256 ? 256 / L : 1;
-            hipLaunchKernelGGL((rn_forward<T, L, S>), dim3(static_cast<unsigned>((plan.R + kRows - 1) / kRows)), dim3(L < 256 ? 256 : L), 0, stream, x,
-                               plan.R, planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+        const auto held = [&](auto lanes, auto slots, auto rows_at_once) {
+            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, J = decltype(rows_at_once)::value, kRows = L < 256 ? 256 / L * J : 1;
+            for (int64_t first = 0; first < plan.R; first += kMostGroups * kRows)
+                hipLaunchKernelGGL((rn_forward<T, L, S, J, false>), dim3(static_cast<unsigned>(std::min((plan.R - first + kRows - 1) / kRows, kMostGroups))),
+                                   dim3(L < 256 ? 256 : L), 0, stream, x, first, plan.R, planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
         };
         const int64_t loads = (n + kPerLoad<T> - 1) / kPerLoad<T>;      // of 16 bytes in a row
         if (plan.parts == 0) {
-            if (loads <= 16) held(Int<16>(), Int<1>());
-            else if (loads <= 64) held(Int<64>(), Int<1>());
-            else if (loads <= 128) held(Int<64>(), Int<2>());
-            else if (loads <= 256) held(Int<64>(), Int<4>());
-            else if (loads <= 512) held(Int<64>(), Int<8>());
-            else if (loads <= 1024) held(Int<256>(), Int<4>());
-            else if (loads <= 2048) held(Int<256>(), Int<8>());
-            else if (loads <= 4096) held(Int<1024>(), Int<4>());
-            else held(Int<1024>(), Int<8>());
+            // lanes to a row, slots, rows at a time: with one slot fewer, or fewer lanes, the row would not fit
+            const int s64 = static_cast<int>((loads + 63) / 64), s256 = static_cast<int>((loads + 255) / 256), s1024 = static_cast<int>((loads + 1023) / 1024);
+            if (loads <= 4) held(Int<4>(), Int<1>(), Int<4>());
+            else if (loads <= 8) held(Int<8>(), Int<1>(), Int<4>());
+            else if (loads <= 16) held(Int<16>(), Int<1>(), Int<4>());
+            else if (loads <= 32) held(Int<32>(), Int<1>(), Int<4>());
+            else if (s64 == 1) held(Int<64>(), Int<1>(), Int<4>());
+            else if (s64 == 2) held(Int<64>(), Int<2>(), Int<2>());
+            else if (s64 == 3) held(Int<64>(), Int<3>(), Int<1>());
+            else if (s64 == 4) held(Int<64>(), Int<4>(), Int<1>());
+            else if (s256 == 2) held(Int<256>(), Int<2>(), Int<1>());
+            else if (s256 == 3) held(Int<256>(), Int<3>(), Int<1>());
+            else if (s256 == 4) held(Int<256>(), Int<4>(), Int<1>());
+            else if (s1024 == 2) held(Int<1024>(), Int<2>(), Int<1>());
+            else if (s1024 == 3) held(Int<1024>(), Int<3>(), Int<1>());
+            else if (s1024 == 4) held(Int<1024>(), Int<4>(), Int<1>());
+            else if (s1024 == 5) held(Int<1024>(), Int<5>(), Int<1>());
+            else if (s1024 == 6) held(Int<1024>(), Int<6>(), Int<1>());
+            else if (s1024 == 7) held(Int<1024>(), Int<7>(), Int<1>());
+            else held(Int<1024>(), Int<8>(), Int<1>());
         } else {
             float4 *moments = static_cast<float4 *>(ws);
             const unsigned tall = static_cast<unsigned>(std::min<int64_t>(plan.R, 32768));
@@ -674,10 +807,10 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
 {
     if (!x_dev || !grad_y_dev || !mean_dev || !rstd_dev || !grad_x_dev) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: NULL pointer");
     if (!rk_type_known(dtype)) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: unknown element type");
-    if (rows < 1 || planes < 1 || n < 1) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: rows, planes and n must be >= 1");
+    if (rows < 1 || planes < 1 || n < 1 || planes > kMostPlanes || n > kMostValues)
+        return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: rows, planes and n must be >= 1, planes <= 65535, n <= 2^30");
     if (misaligned(x_dev, dtype) || misaligned(grad_y_dev, dtype) || misaligned(grad_x_dev, dtype))
         return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: x, grad_y or grad_x is not at an element's address");
-    if (planes > 65535) return rk_fail(ROCKET_EINVAL, "rocket_layer_norm_backward: more than 65535 planes");
     const BackwardPlan plan(rows, planes, n, dtype);
     if (!ws || ws_bytes < plan.bytes() || reinterpret_cast<uintptr_t>(ws) % 16 != 0)
         return rk_fail(ROCKET_EWORKSPACE, "rocket_layer_norm_backward: an aligned workspace of " + std::to_string(plan.bytes()) + " bytes required");
@@ -692,17 +825,21 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
         const auto held = [&](auto lanes, auto slots) {
             constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, G = L < 256 ? 256 / L : 1;
             if (plan.lanes != L || plan.slots != S) return;
-            hipLaunchKernelGGL((rn_backward<T, L, S, G>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)), dim3(L * G), 0, stream, x, dy,
+            hipLaunchKernelGGL((rn_backward<T, L, S, G, true>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)), dim3(L * G), 0, stream, x, dy,
                                rows, planes, n, weight_dev, mean_dev, rstd_dev, dx, part, grad_weight_dev, grad_bias_dev);
         };
+        held(Int<4>(), Int<1>());
+        held(Int<8>(), Int<1>());
         held(Int<16>(), Int<1>());
+        held(Int<32>(), Int<1>());
         held(Int<64>(), Int<1>());
         held(Int<64>(), Int<2>());
         held(Int<256>(), Int<1>());
-        held(Int<256>(), Int<2>());
-        held(Int<512>(), Int<2>());
+        held(Int<512>(), Int<1>());
+        held(Int<1024>(), Int<1>());
         held(Int<1024>(), Int<2>());
         if constexpr (sizeof(T) == 4) {
+            held(Int<1024>(), Int<3>());
             held(Int<1024>(), Int<4>());
             held(Int<1024>(), Int<5>());
         }
@@ -716,7 +853,7 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
         if (part) {
             const int64_t floats = 2 * rn_stride(plan.wide);
             if (floats >= 64 * 512)
-                hipLaunchKernelGGL(rn_backward_finish<64>, dim3(static_cast<unsigned>((floats + 63) / 64)), dim3(kNormThreads), 0, stream, part, plan.parts,
+                hipLaunchKernelGGL(rn_backward_finish<64>, dim3(static_cast<unsigned>(std::min(kMostGroups, (floats + 63) / 64))), dim3(kNormThreads), 0, stream, part, plan.parts,
                                    plan.wide, grad_weight_dev, grad_bias_dev);
             else
                 hipLaunchKernelGGL(rn_backward_finish<16>, dim3(static_cast<unsigned>((floats + 15) / 16)), dim3(kNormThreads), 0, stream, part, plan.parts,

@@ -1,18 +1,20 @@
 // Many tensors at once for MI355X (gfx950): the global norm of all gradients, clipping, and the update that clips on the way.
 // See include/rocket.h for the contract.
 //
-// The tensors of a list are cut into chunks of equal size; the records of up to kPerLaunch tensors travel in a launch's
-// arguments, so nothing is copied to the device beforehand.  A workgroup finds a chunk's tensor by comparing the
-// chunk's number with the first chunks of all tensors, one per lane.
-//   rt_squares   sums of squares of the chunks, fp64: a partial sum per workgroup
+// The values of a list are counted in units of kUnit, each tensor beginning a new one; the workgroups of a launch take every
+// gridDim.x-th unit.  The records of the tensors travel in a launch's arguments, as many as fit 4 KB, so nothing is copied to the
+// device beforehand; a workgroup finds a unit's tensor by comparing its number with the first units of all tensors, one per lane.
+//   rt_squares   sums of squares, fp64: a partial sum per workgroup
 //   rt_finish    norm = sqrt(sum of the partial sums), coefficient = norm <= max ? 1 : max / norm
 //   rt_scale     out = grad * coefficient
 //   rt_sgd       out = param - lr * coefficient * grad
+// All are bound by memory.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "rocket_elements.hpp"
 #include "rocket_internal.hpp"
@@ -20,43 +22,66 @@
 namespace {
 
 constexpr int kThreads_ = 256;
-constexpr int kPerLaunch = 96;            // records of a launch: under 4 KB of arguments with three addresses each
-constexpr int kMostGroups = 2048;         // workgroups of a launch, eight to a CU
+// Values of a unit: of the norm and the scaling 16 KB, four loads of a lane (16-bit values in units of 8 KB: 100 million 56 us, so XX);
+// of the update as many as there are fp32 parameters in 16 KB.
+constexpr int kUnitBytes = 16384;
+template <class T>
+constexpr int kUnit = kUnitBytes / static_cast<int>(sizeof(T));
+constexpr int kSgdUnit = kUnit<float>;
+constexpr int kMostSums = 2048;           // workgroups of all rt_squares over a list together, eight to a CU
+constexpr int kMostGroups = 1 << 20;      // of another launch (its lanes must be fewer than 2^32)
+constexpr int kJoinedSums = 1024;         // partial sums up to which every workgroup of rt_scale adds them up itself: no rt_finish
 
-// Up to kPerLaunch tensors, POINTERS addresses each.
-template <int POINTERS>
+// Tensors of a launch, with POINTERS addresses each: a few, or as many as the arguments may hold.
+constexpr int kFew = 16;
+constexpr int most_records(int pointers) { return (4096 - 128) / (8 * pointers + 4 + 2 + 1); }
+template <int POINTERS, int MOST>
 struct Records {
-    int64_t count[kPerLaunch];
-    void *data[POINTERS][kPerLaunch];
-    int32_t first[kPerLaunch + 1];        // chunk of the launch that a tensor begins with; first[tensors]: chunks of the launch
-    uint8_t dtype[kPerLaunch];
-    int32_t tensors, chunk;               // chunk: values of a chunk, a multiple of 8 * kThreads_
+    static constexpr int kMost = MOST;
+    void *data[POINTERS][kMost];
+    int32_t first[kMost + 1];             // unit of the launch that a tensor begins with; first[tensors]: units of the launch
+    uint16_t tail[kMost];                 // values of its last unit, less one
+    uint8_t dtype[kMost];
+    int32_t tensors;
 };
-
-// The tensor of chunk c: as many lanes as have a tensor that starts at or before c.
 template <int P>
-__device__ __forceinline__ int tensor_of(const Records<P> &r, int c)
+using Many = Records<P, most_records(P)>;
+static_assert(sizeof(Many<1>) <= 4000 && sizeof(Many<2>) <= 4000 && sizeof(Many<3>) <= 4000, "beside the other arguments");
+
+// The tensor of unit u: as many lanes as have a tensor that starts at or before u.
+template <int P, int M>
+__device__ __forceinline__ int tensor_of(const Records<P, M> &r, int u)
 {
     int found = 0;
     for (int i = 0; i < r.tensors; i += 64) {
         const int at = i + static_cast<int>(threadIdx.x & 63);
-        found += __popcll(__ballot(at < r.tensors && r.first[min(at, kPerLaunch)] <= c));
+        found += __popcll(__ballot(at < r.tensors && r.first[min(at, M)] <= u));
     }
     return __builtin_amdgcn_readfirstlane(found - 1);
 }
 
-template <class T>
-__device__ double chunk_squares(const T *g, int64_t count)
+// f(type, whole, tensor, first value, values) for the units of this workgroup.  UNIT: values of a unit, 0: kUnit of the type
+template <int UNIT, int P, int M, class F>
+__device__ __forceinline__ void each_unit(const Records<P, M> &r, F f)
 {
-    constexpr int N = kPerLoad<T>;
-    double s = 0.0;
-    for (int64_t i = static_cast<int64_t>(threadIdx.x) * N; i < count; i += kThreads_ * N) {
-        float v[N];
-        rk_load(g + i, count - i, v);
-#pragma unroll
-        for (int q = 0; q < N; ++q) s = fma(static_cast<double>(v[q]), static_cast<double>(v[q]), s);
+    const int units = r.first[r.tensors];
+    int t = 0, begin = 0, end = 0;
+    for (int u = static_cast<int>(blockIdx.x); u < units; u += static_cast<int>(gridDim.x)) {
+        if (u < begin || u >= end) {
+            t = tensor_of(r, u);
+            begin = r.first[t];
+            end = r.first[t + 1];
+        }
+        const auto one = [&](auto type) {
+            constexpr int kValues = UNIT > 0 ? UNIT : kUnit<decltype(type)>;
+            const int values = u + 1 == end ? static_cast<int>(r.tail[t]) + 1 : kValues;
+            if (values == kValues) f(type, std::true_type(), t, static_cast<int64_t>(u - begin) * kValues, kValues);
+            else f(type, std::false_type(), t, static_cast<int64_t>(u - begin) * kValues, values);
+        };
+        if (r.dtype[t] == ROCKET_F32) one(float());
+        else if (r.dtype[t] == ROCKET_BF16) one(rk_bf16());
+        else one(rk_f16());
     }
-    return s;
 }
 
 __device__ __forceinline__ double group_sum(double v, double *lds)
@@ -69,102 +94,144 @@ __device__ __forceinline__ double group_sum(double v, double *lds)
     return v;
 }
 
-__global__ __launch_bounds__(kThreads_) void rt_squares(const Records<1> r, double *__restrict__ partial)
+// A unit's values from p on; i: this lane's first.  whole: a true_type or a false_type, so that whole units and the last of a tensor
+// have code of their own (where their ways meet again, loads would be waited for).
+template <class T, bool STREAM, int LOADS, class F>
+__device__ __forceinline__ void load_unit(const T *p, int i, int step, int values, F whole, typename RkSlot<T>::V (&v)[LOADS])
+{
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) v[k] = whole ? rk_load_slot<T, STREAM>(p + i + k * step) : rk_load_edge<T, STREAM, true>(p, i + k * step, values);
+}
+
+// STREAM: the list is too long for the caches to keep until the next pass over it
+template <bool STREAM, class R>
+__global__ __launch_bounds__(kThreads_) void rt_squares(const R r, double *__restrict__ partial)
 {
     __shared__ double lds[kThreads_ / 64];
     double s = 0.0;
-    for (int c = blockIdx.x; c < r.first[r.tensors]; c += gridDim.x) {
-        const int t = tensor_of(r, c);
-        const int64_t at = static_cast<int64_t>(c - r.first[t]) * r.chunk, left = min(r.count[t] - at, static_cast<int64_t>(r.chunk));
-        if (r.dtype[t] == ROCKET_F32) s += chunk_squares(static_cast<const float *>(r.data[0][t]) + at, left);
-        else if (r.dtype[t] == ROCKET_BF16) s += chunk_squares(static_cast<const rk_bf16 *>(r.data[0][t]) + at, left);
-        else s += chunk_squares(static_cast<const rk_f16 *>(r.data[0][t]) + at, left);
-    }
+    each_unit<0>(r, [&](auto type, auto whole, int t, int64_t at, int values) {
+        using T = decltype(type);
+        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
+        const T *g = static_cast<const T *>(r.data[0][t]) + at;
+        const int i = static_cast<int>(threadIdx.x) * N;
+        typename RkSlot<T>::V v[kLoads];
+        load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const double d = static_cast<double>(static_cast<float>(v[k][q]));
+                s = fma(d, d, s);
+            }
+    });
     s = group_sum(s, lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+// {norm, coefficient} from the partial sums, in a fixed order
+__device__ __forceinline__ double2 norm_of(const double *partial, int count, double max_norm, double *lds)
+{
+    double s = 0.0;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < count; i += kThreads_) s += partial[i];
+    const double norm = sqrt(group_sum(s, lds));
+    return make_double2(norm, norm <= max_norm ? 1.0 : max_norm / norm);       // NaN stays NaN
 }
 
 __global__ __launch_bounds__(kThreads_) void rt_finish(const double *__restrict__ partial, int count, double max_norm, double *__restrict__ out)
 {
     __shared__ double lds[kThreads_ / 64];
-    double s = 0.0;
-    for (int i = threadIdx.x; i < count; i += kThreads_) s += partial[i];
-    s = group_sum(s, lds);
+    const double2 n = norm_of(partial, count, max_norm, lds);
     if (threadIdx.x == 0) {
-        const double norm = sqrt(s);
-        out[0] = norm;
-        out[1] = norm <= max_norm ? 1.0 : max_norm / norm;     // NaN stays NaN
+        out[0] = n.x;
+        out[1] = n.y;
     }
 }
 
-template <class T>
-__device__ void chunk_scale(const T *g, T *out, int64_t count, double c)
+// r.data: gradients, results.  count > 0: the norm is still in `count` partial sums, which every workgroup adds up; workgroup 0
+// writes it.
+template <bool STREAM, class R>
+__global__ __launch_bounds__(kThreads_) void rt_scale(const R r, const double *__restrict__ partial, int count, double max_norm, double *__restrict__ norm,
+                                                      int in_place)
 {
-    constexpr int N = kPerLoad<T>;
-    for (int64_t i = static_cast<int64_t>(threadIdx.x) * N; i < count; i += kThreads_ * N) {
-        float v[N];
-        rk_load(g + i, count - i, v);
-        // the product in fp64: the coefficient of a norm beyond 1e38 would lose its digits in fp32
+    __shared__ double lds[kThreads_ / 64];
+    double c;
+    if (count > 0) {
+        const double2 n = norm_of(partial, count, max_norm, lds);
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            norm[0] = n.x;
+            norm[1] = n.y;
+        }
+        c = n.y;
+    } else {
+        c = norm[1];
+    }
+    if (in_place && c == 1.0) return;
+    each_unit<0>(r, [&](auto type, auto whole, int t, int64_t at, int values) {
+        using T = decltype(type);
+        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
+        const T *g = static_cast<const T *>(r.data[0][t]) + at;
+        T *o = static_cast<T *>(r.data[1][t]) + at;
+        const int i = static_cast<int>(threadIdx.x) * N;
+        typename RkSlot<T>::V v[kLoads];
+        load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
 #pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = static_cast<float>(static_cast<double>(v[q]) * c);
-        rk_store(out + i, count - i, v);
-    }
-}
-
-// r.data: gradients, results
-__global__ __launch_bounds__(kThreads_) void rt_scale(const Records<2> r, const double *__restrict__ norm, int in_place)
-{
-    const double k = norm[1];
-    if (in_place && k == 1.0) return;
-    for (int c = blockIdx.x; c < r.first[r.tensors]; c += gridDim.x) {
-        const int t = tensor_of(r, c);
-        const int64_t at = static_cast<int64_t>(c - r.first[t]) * r.chunk, left = min(r.count[t] - at, static_cast<int64_t>(r.chunk));
-        if (r.dtype[t] == ROCKET_F32) chunk_scale(static_cast<const float *>(r.data[0][t]) + at, static_cast<float *>(r.data[1][t]) + at, left, k);
-        else if (r.dtype[t] == ROCKET_BF16) chunk_scale(static_cast<const rk_bf16 *>(r.data[0][t]) + at, static_cast<rk_bf16 *>(r.data[1][t]) + at, left, k);
-        else chunk_scale(static_cast<const rk_f16 *>(r.data[0][t]) + at, static_cast<rk_f16 *>(r.data[1][t]) + at, left, k);
-    }
-}
-
-template <class T>
-__device__ void chunk_sgd(const float *p, const T *g, float *out, int64_t count, double rate)
-{
-    constexpr int N = 4;
-    for (int64_t i = static_cast<int64_t>(threadIdx.x) * N; i < count; i += kThreads_ * N) {
-        float v[N], w[N];
-        rk_load(p + i, count - i, v);
-        for (int q = 0; q < N; ++q) w[q] = i + q < count ? static_cast<float>(g[i + q]) : 0.f;
+        for (int k = 0; k < kLoads; ++k) {
+            // the product in fp64: the coefficient of a norm beyond 1e38 would lose its digits in fp32
+            float u[N];
 #pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = static_cast<float>(fma(-rate, static_cast<double>(w[q]), static_cast<double>(v[q])));
-        rk_store(out + i, count - i, v);
-    }
+            for (int q = 0; q < N; ++q) u[q] = static_cast<float>(static_cast<double>(static_cast<float>(v[k][q])) * c);
+            rk_store<T, true>(o + i + k * kStep, whole ? N : values - i - k * kStep, u);
+        }
+    });
 }
 
 // r.data: gradients, parameters, results
-__global__ __launch_bounds__(kThreads_) void rt_sgd(const Records<3> r, double lr, const double *__restrict__ norm)
+template <bool STREAM, class R>
+__global__ __launch_bounds__(kThreads_) void rt_sgd(const R r, double lr, const double *__restrict__ norm)
 {
     const double rate = norm ? lr * norm[1] : lr;
-    for (int c = blockIdx.x; c < r.first[r.tensors]; c += gridDim.x) {
-        const int t = tensor_of(r, c);
-        const int64_t at = static_cast<int64_t>(c - r.first[t]) * r.chunk, left = min(r.count[t] - at, static_cast<int64_t>(r.chunk));
+    each_unit<kSgdUnit>(r, [&](auto type, auto whole, int t, int64_t at, int values) {
+        using T = decltype(type);
+        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kSgdUnit / kStep;
+        const T *g = static_cast<const T *>(r.data[0][t]) + at;
         const float *p = static_cast<const float *>(r.data[1][t]) + at;
-        float *out = static_cast<float *>(r.data[2][t]) + at;
-        if (r.dtype[t] == ROCKET_F32) chunk_sgd(p, static_cast<const float *>(r.data[0][t]) + at, out, left, rate);
-        else if (r.dtype[t] == ROCKET_BF16) chunk_sgd(p, static_cast<const rk_bf16 *>(r.data[0][t]) + at, out, left, rate);
-        else chunk_sgd(p, static_cast<const rk_f16 *>(r.data[0][t]) + at, out, left, rate);
-    }
+        float *o = static_cast<float *>(r.data[2][t]) + at;
+        const int i = static_cast<int>(threadIdx.x) * N;
+        typename RkSlot<T>::V v[kLoads];
+        RkSlot<float>::V w[kLoads * N / 4];
+        load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
+        // the parameters of a lane's values: N of them from i + k * kStep on
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+#pragma unroll
+            for (int q = 0; q < N; q += 4) {
+                const int j = i + k * kStep + q;
+                w[(k * N + q) / 4] = whole ? rk_load_slot<float, true>(p + j) : rk_load_edge<float, true, true>(p, j, values);
+            }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            float u[N];
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                u[q] = static_cast<float>(fma(-rate, static_cast<double>(static_cast<float>(v[k][q])), static_cast<double>(w[(k * N + q) / 4][q % 4])));
+            rk_store_f32<N, true>(o + i + k * kStep, whole ? N : values - i - k * kStep, u);
+        }
+    });
 }
 
-constexpr int64_t kMostValues = int64_t{1} << 42;      // of one tensor: chunk numbers stay below 2^31 with room for a launch's tensors
+constexpr int64_t kMostValues = int64_t{1} << 40;      // of a list: units stay below 2^30
 
 // "" or what is wrong with a list
 std::string list_fault(const rocket_tensor *t, int32_t tensors, bool f32_only)
 {
     if (!t) return "NULL list";
     if (tensors < 1) return "a list holds one tensor at least";
+    int64_t values = 0;
     for (int32_t i = 0; i < tensors; ++i) {
         const char *what = nullptr;
         if (!rk_type_known(t[i].dtype) || (f32_only && t[i].dtype != ROCKET_F32)) what = f32_only ? "ROCKET_F32 required" : "unknown element type";
-        else if (t[i].count < 0 || t[i].count > kMostValues) what = "a count outside [0, 2^42]";
+        else if (t[i].count < 0 || t[i].count > kMostValues || (values += t[i].count) > kMostValues) what = "a negative count, or more than 2^40 values";
         else if (t[i].count > 0 && !t[i].data) what = "NULL data";
         else if (t[i].count > 0 && reinterpret_cast<uintptr_t>(t[i].data) % rk_type_bytes(t[i].dtype) != 0) what = "not at an element's address";
         if (what) return "tensor " + std::to_string(i) + ": " + what;
@@ -180,86 +247,94 @@ std::string pair_fault(const rocket_tensor *a, const rocket_tensor *b, int32_t t
     return "";
 }
 
-// Chunks so large that all tensors together make about kMostGroups of them, between 2,048 and 16,384 values; the chunks of a
-// launch must fit 31 bits (larger ones where they would not).
+inline int64_t unit_of(int32_t dtype) { return kUnitBytes / static_cast<int64_t>(rk_type_bytes(dtype)); }
+
+// A list's launches.
 struct ListPlan {
-    int32_t chunk = 0, launches = 0;
-    int64_t groups = 0;      // workgroups of all launches
-    ListPlan(const rocket_tensor *t, int32_t tensors)
+    int64_t units = 0, bytes = 0, unit;
+    // unit: values of one, 0: kUnit of each tensor's type
+    ListPlan(const rocket_tensor *t, int32_t tensors, int64_t unit = 0) : unit(unit)
     {
-        int64_t values = 0;
-        for (int32_t i = 0; i < tensors; ++i) values += t[i].count;
-        int64_t c = std::min<int64_t>(std::max<int64_t>(values / kMostGroups, 2048), 16384) / 2048 * 2048;
-        while (values / c > (int64_t{1} << 30)) c *= 2;
-        chunk = static_cast<int32_t>(std::min<int64_t>(c, 1 << 30));
-        each(t, tensors, [&](int32_t, int32_t, int64_t chunks) {
-            ++launches;
-            groups += std::min<int64_t>(chunks, kMostGroups);
-            return ROCKET_OK;
-        });
+        for (int32_t i = 0; i < tensors; ++i) {
+            units += units_of(t[i]);
+            bytes += t[i].count * static_cast<int64_t>(rk_type_bytes(t[i].dtype));
+        }
     }
-    int64_t chunks_of(int64_t count) const { return (count + chunk - 1) / chunk; }
-    // f(first tensor, one past the last, chunks) for the tensors of each launch
-    template <class F>
-    int each(const rocket_tensor *t, int32_t tensors, F f) const
+    int64_t values(const rocket_tensor &t) const { return unit > 0 ? unit : unit_of(t.dtype); }
+    int64_t units_of(const rocket_tensor &t) const { return (t.count + values(t) - 1) / values(t); }
+    // f(records, units) for each launch of tensors with P addresses each; a list without values has none
+    template <int P, class F>
+    int each(const rocket_tensor *const (&lists)[P], int32_t tensors, F f) const
     {
-        for (int32_t a = 0; a < tensors;) {
-            int64_t chunks = 0;
-            int32_t b = a;
-            int filled = 0;
-            for (; b < tensors && filled < kPerLaunch; ++b) {
-                const int64_t more = chunks_of(t[b].count);
-                if (chunks + more > INT32_MAX - kMostGroups && chunks > 0) break;
-                chunks += more;
-                filled += more > 0;
+        return tensors <= kFew ? each_of<Records<P, kFew>>(lists, tensors, f) : each_of<Many<P>>(lists, tensors, f);
+    }
+    template <class R, int P, class F>
+    int each_of(const rocket_tensor *const (&lists)[P], int32_t tensors, F f) const
+    {
+        for (int32_t i = 0; i < tensors;) {
+            R r;
+            int k = 0;
+            int64_t some = 0;
+            for (; i < tensors && k < R::kMost; ++i) {
+                const int64_t count = lists[0][i].count;
+                if (count == 0) continue;
+                for (int p = 0; p < P; ++p) r.data[p][k] = lists[p][i].data;
+                r.first[k] = static_cast<int32_t>(some);
+                r.tail[k] = static_cast<uint16_t>((count - 1) % values(lists[0][i]));
+                r.dtype[k++] = static_cast<uint8_t>(lists[0][i].dtype);
+                some += units_of(lists[0][i]);
             }
-            if (chunks > 0)
-                if (const int rc = f(a, b, chunks); rc != ROCKET_OK) return rc;
-            a = b;
+            if (k == 0) break;
+            r.first[k] = static_cast<int32_t>(some);
+            r.tensors = k;
+            const int rc = f(r, some);
+            if (rc != ROCKET_OK) return rc;
         }
         return ROCKET_OK;
     }
-};
-
-template <int P>
-void fill(Records<P> &r, const ListPlan &plan, int32_t a, int32_t b, const rocket_tensor *const (&lists)[P])
-{
-    int k = 0;
-    int64_t first = 0;
-    for (int32_t i = a; i < b; ++i) {
-        const int64_t count = lists[0][i].count;
-        if (count == 0) continue;
-        r.count[k] = count;
-        r.dtype[k] = static_cast<uint8_t>(lists[0][i].dtype);
-        for (int p = 0; p < P; ++p) r.data[p][k] = lists[p][i].data;
-        r.first[k++] = static_cast<int32_t>(first);
-        first += plan.chunks_of(count);
+    // partial sums of a launch of a norm: of kMostSums as many as it has of the units
+    int64_t sums(int64_t some) const { return std::min(some, std::max<int64_t>(1, kMostSums * some / units)); }
+    size_t workspace(int32_t tensors) const
+    {
+        const int64_t most = std::min<int64_t>(units, kMostSums + tensors / Many<1>::kMost + 1);
+        return static_cast<size_t>((most * 8 + 255) / 256 * 256 + 256);
     }
-    r.first[k] = static_cast<int32_t>(first);
-    r.tensors = k;
-    r.chunk = plan.chunk;
-}
+};
 
 int checked_launch(const char *who)
 {
     return hipGetLastError() == hipSuccess ? ROCKET_OK : rk_fail(ROCKET_EHIP, std::string(who) + ": launch of a kernel failed");
 }
 
-int norm_impl(const char *who, const rocket_tensor *grads, int32_t tensors, double max_norm, double *norm_dev, void *ws, size_t ws_bytes,
-              hipStream_t stream, const ListPlan &plan)
+unsigned groups_of(int64_t units) { return static_cast<unsigned>(std::min<int64_t>(units, kMostGroups)); }
+
+// What a pass leaves for the next one is kept by the caches up to here (256 MB on the memory's side); beyond, or on the way out, it
+// only displaces.
+constexpr int64_t kKeptBytes = 192 << 20;
+template <class F>
+void by_length(bool stream, F f)
 {
-    double *partial = static_cast<double *>(ws);
-    int64_t at = 0;
-    const int rc = plan.each(grads, tensors, [&](int32_t a, int32_t b, int64_t chunks) {
-        Records<1> r;
-        fill<1>(r, plan, a, b, {grads});
-        const unsigned groups = static_cast<unsigned>(std::min<int64_t>(chunks, kMostGroups));
-        hipLaunchKernelGGL(rt_squares, dim3(groups), dim3(kThreads_), 0, stream, r, partial + at);
-        at += groups;
+    if (stream) f(std::true_type());
+    else f(std::false_type());
+}
+
+// the partial sums of a norm; *count receives their number
+int squares(const char *who, const rocket_tensor *grads, int32_t tensors, double *partial, hipStream_t stream, const ListPlan &plan, int *count)
+{
+    *count = 0;
+    return plan.each<1>({grads}, tensors, [&](const auto &r, int64_t units) {
+        const int sums = static_cast<int>(plan.sums(units));
+        by_length(plan.bytes > kKeptBytes, [&](auto once) {
+            hipLaunchKernelGGL((rt_squares<decltype(once)::value>), dim3(static_cast<unsigned>(sums)), dim3(kThreads_), 0, stream, r, partial + *count);
+        });
+        *count += sums;
         return checked_launch(who);
     });
-    if (rc != ROCKET_OK) return rc;
-    hipLaunchKernelGGL(rt_finish, dim3(1), dim3(kThreads_), 0, stream, partial, static_cast<int>(at), max_norm, norm_dev);
+}
+
+int finish(const char *who, const double *partial, int count, double max_norm, double *norm_dev, hipStream_t stream)
+{
+    hipLaunchKernelGGL(rt_finish, dim3(1), dim3(kThreads_), 0, stream, partial, count, max_norm, norm_dev);
     return checked_launch(who);
 }
 
@@ -280,17 +355,18 @@ int check_norm(const char *fn, const rocket_tensor *grads, int32_t tensors, doub
 
 extern "C" size_t rocket_grad_workspace_bytes(const rocket_tensor *grads, int32_t tensors)
 {
-    if (!list_fault(grads, tensors, false).empty()) return 0;
-    const ListPlan plan(grads, tensors);
-    return static_cast<size_t>((plan.groups * 8 + 255) / 256 * 256 + 256);
+    return list_fault(grads, tensors, false).empty() ? ListPlan(grads, tensors).workspace(tensors) : 0;
 }
 
 extern "C" int rocket_grad_norm(const rocket_tensor *grads, int32_t tensors, double max_norm, double *norm_dev, void *ws, size_t ws_bytes,
                                 void *hip_stream)
 {
-    if (const int rc = check_norm("rocket_grad_norm", grads, tensors, max_norm, norm_dev, ws, ws_bytes); rc != ROCKET_OK) return rc;
-    return norm_impl("rocket_grad_norm", grads, tensors, max_norm, norm_dev, ws, ws_bytes, static_cast<hipStream_t>(hip_stream),
-                     ListPlan(grads, tensors));
+    const char *who = "rocket_grad_norm";
+    if (const int rc = check_norm(who, grads, tensors, max_norm, norm_dev, ws, ws_bytes); rc != ROCKET_OK) return rc;
+    double *partial = static_cast<double *>(ws);
+    int count = 0;
+    if (const int rc = squares(who, grads, tensors, partial, static_cast<hipStream_t>(hip_stream), ListPlan(grads, tensors), &count); rc != ROCKET_OK) return rc;
+    return finish(who, partial, count, max_norm, norm_dev, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor *out, int32_t tensors, double max_norm, double *norm_dev, void *ws,
@@ -305,12 +381,17 @@ extern "C" int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor 
     }
     const ListPlan plan(grads, tensors);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (const int rc = norm_impl(who, grads, tensors, max_norm, norm_dev, ws, ws_bytes, stream, plan); rc != ROCKET_OK) return rc;
-    return plan.each(grads, tensors, [&](int32_t a, int32_t b, int64_t chunks) {
-        Records<2> r;
-        fill<2>(r, plan, a, b, {grads, out ? out : grads});
-        hipLaunchKernelGGL(rt_scale, dim3(static_cast<unsigned>(std::min<int64_t>(chunks, kMostGroups))), dim3(kThreads_), 0, stream, r, norm_dev,
-                           out ? 0 : 1);
+    double *partial = static_cast<double *>(ws);
+    int count = 0;
+    int rc = squares(who, grads, tensors, partial, stream, plan, &count);
+    const bool joined = count <= kJoinedSums && plan.units > 0;
+    if (rc == ROCKET_OK && !joined) rc = finish(who, partial, count, max_norm, norm_dev, stream);
+    if (rc != ROCKET_OK) return rc;
+    return plan.each<2>({grads, out ? out : grads}, tensors, [&](const auto &r, int64_t units) {
+        by_length(plan.bytes > kKeptBytes, [&](auto once) {
+            hipLaunchKernelGGL((rt_scale<decltype(once)::value>), dim3(groups_of(units)), dim3(kThreads_), 0, stream, r, partial, joined ? count : 0, max_norm,
+                               norm_dev, out ? 0 : 1);
+        });
         return checked_launch(who);
     });
 }
@@ -326,12 +407,11 @@ extern "C" int rocket_sgd_tensors(const rocket_tensor *params, const rocket_tens
     if (fault.empty() && out) fault = pair_fault(grads, out, tensors, false);
     if (!fault.empty()) return rk_fail(ROCKET_EINVAL, who + fault);
     if (!std::isfinite(lr)) return rk_fail(ROCKET_EINVAL, who + "lr must be finite");
-    const ListPlan plan(grads, tensors);
-    return plan.each(grads, tensors, [&](int32_t a, int32_t b, int64_t chunks) {
-        Records<3> r;
-        fill<3>(r, plan, a, b, {grads, params, out ? out : params});
-        hipLaunchKernelGGL(rt_sgd, dim3(static_cast<unsigned>(std::min<int64_t>(chunks, kMostGroups))), dim3(kThreads_), 0,
-                           static_cast<hipStream_t>(hip_stream), r, lr, norm_dev);
+    const ListPlan plan(grads, tensors, kSgdUnit);
+    return plan.each<3>({grads, params, out ? out : params}, tensors, [&](const auto &r, int64_t units) {
+        by_length(plan.bytes > kKeptBytes, [&](auto once) {
+            hipLaunchKernelGGL((rt_sgd<decltype(once)::value>), dim3(groups_of(units)), dim3(kThreads_), 0, static_cast<hipStream_t>(hip_stream), r, lr, norm_dev);
+        });
         return checked_launch("rocket_sgd_tensors");
     });
 }

@@ -18,7 +18,7 @@ def test_layer_norm_refusals():
     def norm(x=P, dtype=0, rows=4, planes=2, n=30, eps=1e-5, y=P, mean=None, rstd=None, ws=P, size=BIG):
         return lib.rocket_layer_norm(x, dtype, rows, planes, n, P, P, eps, y, mean, rstd, ws, size, None)
 
-    for bad in (dict(x=None), dict(y=None), dict(dtype=3), dict(dtype=-1), dict(rows=0), dict(planes=0), dict(n=0), dict(n=-5), dict(eps=0.0),
+    for bad in (dict(x=None), dict(y=None), dict(dtype=3), dict(dtype=-1), dict(rows=0), dict(planes=0), dict(n=0), dict(n=-5), dict(planes=65536), dict(n=2**30 + 1), dict(eps=0.0),
                 dict(eps=-1.0), dict(eps=float("inf")), dict(eps=float("nan")), dict(mean=P), dict(rstd=P), dict(x=ctypes.c_void_p(4098)),
                 dict(y=ctypes.c_void_p(4097), dtype=1)):
         assert norm(**bad) == E, bad
@@ -38,16 +38,19 @@ def test_layer_norm_refusals():
         assert lib.rocket_layer_norm_workspace_bytes(*sizes, 0) == 0 and lib.rocket_layer_norm_workspace_bytes(*sizes, 1) == 0
 
 
-@pytest.mark.parametrize("rows,planes,n", [(1, 1, 2**31 - 1), (2**31 - 1, 1, 1), (2**31 - 1, 3, 2**31 - 1), (65535, 65535, 100), (1, 2**31 - 1, 7)])
+@pytest.mark.parametrize("rows,planes,n", [(1, 1, 2**30), (2**31 - 1, 1, 1), (2**31 - 1, 3, 2**30), (65535, 65535, 100), (1, 2**31 - 1, 7), (1, 1, 2**30 + 1)])
 def test_workspace_sizes_do_not_wrap(rows, planes, n):
     """sizes are 64-bit throughout: more rows or values never need less"""
     lib = rocket.load_library()
     for backward in (0, 1):
         need = lib.rocket_layer_norm_workspace_bytes(rows, planes, n, backward)
-        assert need % 256 == 0
-        assert need >= lib.rocket_layer_norm_workspace_bytes(max(1, rows // 4096), planes, n, backward) or not backward
-        if backward:
-            assert need >= 4 * planes * n       # a partial sum of the weight gradient at least
+        if planes > 65535 or n > 2**30:      # refused by the calls
+            assert need == 0
+            continue
+        assert need % 256 == 0 and (need > 0 or not backward)
+        assert need >= lib.rocket_layer_norm_workspace_bytes(max(1, rows // 4096), planes, n, backward)
+        if n > 1 << 20:         # rows in parts: a record for each
+            assert need >= 16 * rows * planes
 
 
 def _list(*records):
