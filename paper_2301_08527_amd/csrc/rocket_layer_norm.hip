@@ -179,67 +179,80 @@ __device__ __forceinline__ float rn_rstd(const Moments &m, float eps) { return 1
 
 // A row lies in the registers of LANES lanes, SLOTS loads of 16 bytes in each (as loaded: 16-bit values take half the registers),
 // so x is read once.  Two passes over the registers give the mean and the distances from it; up to 64 lanes meet by lane
-// exchanges alone, more lanes once through LDS, where the wavefronts' own means and sums of squares are joined.  Short rows: ROWS
-// of them to each group of lanes, loaded together.  Rows from `first` on.
+// exchanges alone, more lanes once through LDS, where the wavefronts' own means and sums of squares are joined.  A group of lanes has one
+// plane of ROWS examples, whose weights it loads once.  Groups of neighbouring planes lie side by side; examples from
+// `first` on.
 template <class T, int LANES, int SLOTS, int ROWS, bool STREAM>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int64_t first, int64_t R, int planes, int n,
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int first, int rows, int planes, int n,
                                                                         const float *__restrict__ weight, const float *__restrict__ bias, float eps,
                                                                         T *y, float *__restrict__ mean, float *__restrict__ rstd)
 {
     constexpr int N = kPerLoad<T>, kGroups = LANES < 256 ? 256 / LANES : 1;
-    constexpr bool kEarly = ROWS == 1 && SLOTS * N <= 16;       // weights and biases are on their way while the lanes meet
-    static_assert(LANES <= 64 || (ROWS == 1 && LANES >= 256), "a row of several wavefronts has the workgroup to itself");
-    __shared__ float4 meet[LANES > 64 ? 16 : 1];
-    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1);
-    const int64_t row0 = first + static_cast<int64_t>(blockIdx.x) * (kGroups * ROWS) + threadIdx.x / LANES;
+    constexpr bool kEarly = SLOTS * N * (ROWS > 2 ? 2 : ROWS) <= 16;       // weights and biases are on their way while the lanes meet
+    static_assert(LANES <= 64 || LANES >= 256, "a row of several wavefronts has the workgroup to itself");
+    __shared__ float4 meet[LANES > 64 ? ROWS : 1][LANES > 64 ? 16 : 1];
+    const int lane = static_cast<int>(threadIdx.x) & (LANES - 1), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const unsigned group = blockIdx.x * kGroups + threadIdx.x / LANES, block = group / static_cast<unsigned>(planes);
+    const int plane = static_cast<int>(group - block * static_cast<unsigned>(planes));
+    const int64_t b0 = first + static_cast<int64_t>(block) * ROWS;
+    if (LANES <= 64 && b0 >= rows) return;
     const Place<T, LANES, SLOTS> place(n, lane);
     Held<T, SLOTS> raw[ROWS];
     float w[kEarly ? SLOTS : 1][N], b[kEarly ? SLOTS : 1][N];
-    const auto load_beside = [&](int64_t w0, int k, float (&ww)[N], float (&bb)[N]) {
+    const int64_t w0 = static_cast<int64_t>(plane) * n;
+    const auto load_beside = [&](int k, float (&ww)[N], float (&bb)[N]) {
 #pragma unroll
         for (int q = 0; q < N; ++q) ww[q] = 1.f, bb[q] = 0.f;
         if (weight) rn_beside(weight + w0, place, k, ww);
         if (bias) rn_beside(bias + w0, place, k, bb);
     };
+    const auto row_of = [&](int j) { return min(b0 + j, static_cast<int64_t>(rows) - 1) * planes + plane; };       // beyond the last: the last once more
 #pragma unroll
-    for (int j = 0; j < ROWS; ++j)      // rows beyond the last: the last once more
-        rn_hold<T, LANES, SLOTS, STREAM>(raw[j], x + min(row0 + j * kGroups, R - 1) * n, place);
+    for (int j = 0; j < ROWS; ++j) rn_hold<T, LANES, SLOTS, STREAM>(raw[j], x + row_of(j) * n, place);
     if constexpr (kEarly)
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k) load_beside(min(row0, R - 1) % planes * n, k, w[k], b[k]);
+        for (int k = 0; k < SLOTS; ++k) load_beside(k, w[k], b[k]);
     const auto counts = [&](int k, int q) { return place.counts(k, q); };
+    Moments m[ROWS];
+    float r[ROWS];
+    if constexpr (LANES <= 64) {
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) m[j] = rn_moments<T, LANES, SLOTS>(raw[j], static_cast<float>(n), counts);
+    } else {
+        const int count = (SLOTS - 1) * 64 * N + min(max(n - ((SLOTS - 1) * place.kStep + wave * 64 * N), 0), 64 * N);
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            const Moments own = rn_moments<T, 64, SLOTS>(raw[j], static_cast<float>(max(count, 1)), counts);
+            if ((threadIdx.x & 63) == 0) meet[j][wave] = make_float4(static_cast<float>(count), own.shift, own.rest, own.m2);
+            if (static_cast<int>(threadIdx.x) >= LANES - 64 && static_cast<int>(threadIdx.x & 63) > 0 && wave + static_cast<int>(threadIdx.x & 63) < 16)
+                meet[j][wave + (threadIdx.x & 63)] = make_float4(0.f, 0.f, 0.f, 0.f);        // places that no wavefront has
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            const float4 part = meet[j][threadIdx.x & 15];
+            m[j] = rn_join({part.x, part.y, part.z, part.w}, static_cast<float>(n));
+        }
+    }
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
-        const int64_t row = row0 + j * kGroups;
-        Moments m;
-        if constexpr (LANES <= 64) {
-            m = rn_moments<T, LANES, SLOTS>(raw[j], static_cast<float>(n), counts);
-        } else {
-            const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-            const int count = (SLOTS - 1) * 64 * N + min(max(n - ((SLOTS - 1) * place.kStep + wave * 64 * N), 0), 64 * N);
-            const Moments own = rn_moments<T, 64, SLOTS>(raw[j], static_cast<float>(max(count, 1)), counts);
-            if ((threadIdx.x & 63) == 0) meet[wave] = make_float4(static_cast<float>(count), own.shift, own.rest, own.m2);
-            if (static_cast<int>(threadIdx.x) >= LANES - 64 && static_cast<int>(threadIdx.x & 63) > 0 && wave + static_cast<int>(threadIdx.x & 63) < 16)
-                meet[wave + (threadIdx.x & 63)] = make_float4(0.f, 0.f, 0.f, 0.f);        // places that no wavefront has
-            __syncthreads();
-            const float4 part = meet[threadIdx.x & 15];
-            m = rn_join({part.x, part.y, part.z, part.w}, static_cast<float>(n));
-        }
-        if (row >= R) continue;
+        r[j] = rn_rstd(m[j], eps);
         if constexpr (sizeof(T) == 2) rn_forget<T, SLOTS>(raw[j]);
-        const float r = rn_rstd(m, eps);
+        if (mean && lane == 0 && b0 + j < rows) {
+            mean[row_of(j)] = m[j].shift + m[j].rest;
+            rstd[row_of(j)] = r[j];
+        }
+    }
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k) {
+    for (int k = 0; k < SLOTS; ++k) {
+        if constexpr (!kEarly) load_beside(k, w[0], b[0]);
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
             float v[N], out[N];
-            if constexpr (!kEarly) load_beside(row % planes * n, k, w[0], b[0]);
 #pragma unroll
             for (int q = 0; q < N; ++q) v[q] = static_cast<float>(raw[j][k][q]);
-            rn_normal(v, m, r, w[kEarly ? k : 0], b[kEarly ? k : 0], out);
-            rn_put<T, LANES, SLOTS, STREAM>(y + row * n, place, k, out);
-        }
-        if (mean && lane == 0) {
-            mean[row] = m.shift + m.rest;
-            rstd[row] = r;
+            rn_normal(v, m[j], r[j], w[kEarly ? k : 0], b[kEarly ? k : 0], out);
+            if (ROWS == 1 || b0 + j < rows) rn_put<T, LANES, SLOTS, STREAM>(y + row_of(j) * n, place, k, out);
         }
     }
 }
@@ -251,14 +264,14 @@ template <class T>
 constexpr int kPart = kNormThreads * kPartSlots * kPerLoad<T>;
 
 // The slots of a piece from value `from` of a row of n on; whole: the row has all of them (else zeros beyond its end)
-template <class T, class F>
+template <class T, bool STREAM, class F>
 __device__ __forceinline__ void rn_piece(Held<T, kPartSlots> &raw, const T *src, int from, int n, F whole)
 {
     constexpr int N = kPerLoad<T>;
 #pragma unroll
     for (int k = 0; k < kPartSlots; ++k) {
         const int i = from + (k * kNormThreads + static_cast<int>(threadIdx.x)) * N;
-        raw[k] = whole ? rk_load_slot<T, false>(src + i) : rk_load_edge<T, false, false>(src, i, n);
+        raw[k] = whole ? rk_load_slot<T, STREAM>(src + i) : rk_load_edge<T, STREAM, false>(src, i, n);
     }
 }
 
@@ -285,7 +298,7 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_parts(const T *x, int
             Moments own;
             rn_by_whole(some == kPart<T>, [&](auto whole) {
                 Held<T, kPartSlots> raw;
-                rn_piece<T>(raw, x + row * n, at, n, whole);
+                rn_piece<T, false>(raw, x + row * n, at, n, whole);
 #pragma unroll
                 for (int k = 0; k < kPartSlots; ++k) count += whole ? 64 * N : min(max(some - (k * kNormThreads * N + wave * 64 * N), 0), 64 * N);
                 own = rn_moments<T, 64, kPartSlots>(raw, static_cast<float>(max(count, 1)), [&](int k, int q) {
@@ -325,7 +338,9 @@ __device__ __forceinline__ Moments rn_row_moments(const float4 *moments, int par
     return m;
 }
 
-template <class T>
+// What is written is never kept for the next kernel at the cost of what the caches hold, what is read for the last time (ONCE) neither where
+// they did not keep it anyway: 1,000 x 50,000 fp32 128 us, so 108; 1,000 x 150,000 347, so 313.
+template <class T, bool ONCE>
 __global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int64_t R, int planes, int n, int length, int parts,
                                                                  const float4 *__restrict__ moments, const float *__restrict__ weight,
                                                                  const float *__restrict__ bias, float eps, T *y, float *__restrict__ mean,
@@ -339,7 +354,7 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int
         const int from = static_cast<int>(blockIdx.x) * kPart<T>;
         rn_by_whole(from + kPart<T> <= n, [&](auto whole) {
             Held<T, kPartSlots> raw;
-            rn_piece<T>(raw, x + row * n, from, n, whole);
+            rn_piece<T, ONCE>(raw, x + row * n, from, n, whole);
 #pragma unroll
             for (int k = 0; k < kPartSlots; ++k) {
                 const int i = from + (k * kNormThreads + static_cast<int>(threadIdx.x)) * N;
@@ -355,7 +370,7 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int
                     else rk_load_f32_edge<N, false>(bias + w0, i, n, b);
                 }
                 rn_normal(v, m, r, w, b, out);
-                if (whole || i < n) rk_store<T, false>(y + row * n + i, whole ? N : n - i, out);
+                if (whole || i < n) rk_store<T, true>(y + row * n + i, whole ? N : n - i, out);
             }
         });
         if (mean && blockIdx.x == 0 && threadIdx.x == 0) {
@@ -380,6 +395,7 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
                                                               float *__restrict__ part, float *__restrict__ grad_w, float *__restrict__ grad_b)
 {
     constexpr int N = kPerLoad<T>, kWaves = LANES > 64 ? LANES / 64 : 1, kWide = SLOTS * N * LANES;
+    constexpr bool kAhead = sizeof(T) == 2 && SLOTS == 1 && LANES >= 256;       // the next row is loaded before the last one is done with
     static_assert(LANES <= 64 || GROUPS == 1, "a row of several wavefronts has the workgroup to itself");
     __shared__ float meet[2][3][kWaves];
     __shared__ float4 total[GROUPS > 1 ? 2 * kWide / 4 : 1];
@@ -398,13 +414,20 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
     if constexpr (kKeep)
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) load_weights(weight, k, kept[k]);
-    int turn = 0;
-    for (int64_t b = static_cast<int64_t>(blockIdx.x) * GROUPS + group; b < rows; b += static_cast<int64_t>(gridDim.x) * GROUPS, turn ^= 1) {
-        const int64_t row = b * planes + plane;
+    struct Row {
         Held<T, SLOTS> xs, ds;
-        rn_hold<T, LANES, SLOTS, STREAM>(xs, x + row * n, place);
-        rn_hold<T, LANES, SLOTS, STREAM>(ds, dy + row * n, place);
-        const float m = mean[row], r = rstd[row];
+        float m, r;
+    };
+    int turn = 0;
+    const auto load_row = [&](Row &row, int64_t b) {       // beyond the last: the last once more
+        const int64_t at = min(b, static_cast<int64_t>(rows) - 1) * planes + plane;
+        rn_hold<T, LANES, SLOTS, STREAM>(row.xs, x + at * n, place);
+        rn_hold<T, LANES, SLOTS, STREAM>(row.ds, dy + at * n, place);
+        row.m = mean[at];
+        row.r = rstd[at];
+    };
+    const auto use_row = [&](Row &row, int64_t b) {
+        const float m = row.m, r = row.r;
         const float *again = weight;
         if constexpr (!kKeep) asm volatile("" : "+s"(again));       // or the loads are moved out of the loop, into registers that are not there
         float s[3] = {0.f, 0.f, 0.f};
@@ -414,7 +437,7 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
             const float (&w)[N] = kept[kKeep ? k : 0];
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
+                const float h = (static_cast<float>(row.xs[k][q]) - m) * r, g = static_cast<float>(row.ds[k][q]) * w[q];
                 const bool count = place.counts(k, q);
                 s[0] += count ? g : 0.f;
                 s[1] += count ? g * h : 0.f;
@@ -431,10 +454,12 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<16>(static_cast<int>(threadIdx.x & 15) < kWaves ? meet[turn][i][threadIdx.x & 15] : 0.f);
+            turn ^= 1;
         }
         const float c1 = s[0] * per, e = s[2] * per, c2 = fmaf(-e, s[0], s[1]) * per;
-        rn_forget<T, SLOTS>(xs);
-        rn_forget<T, SLOTS>(ds);
+        rn_forget<T, SLOTS>(row.xs);
+        rn_forget<T, SLOTS>(row.ds);
+        T *to = dx + (b * planes + plane) * n;
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
             if constexpr (!kKeep) load_weights(again, k, kept[0]);
@@ -442,12 +467,33 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
             float v[N];
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const float h = fmaf(static_cast<float>(xs[k][q]) - m, r, -e), d = static_cast<float>(ds[k][q]);
+                const float h = fmaf(static_cast<float>(row.xs[k][q]) - m, r, -e), d = static_cast<float>(row.ds[k][q]);
                 dw[k][q] = fmaf(d, h, dw[k][q]);
                 db[k][q] += d;
                 v[q] = r * (fmaf(-h, c2, d * w[q]) - c1);
             }
-            rn_put<T, LANES, SLOTS, STREAM>(dx + row * n, place, k, v);
+            rn_put<T, LANES, SLOTS, STREAM>(to, place, k, v);
+        }
+    };
+    int64_t b = static_cast<int64_t>(blockIdx.x) * GROUPS + group;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * GROUPS;
+    if constexpr (kAhead) {
+        Row one, two;
+        if (b < rows) load_row(one, b);
+        while (b < rows) {
+            load_row(two, b + stride);
+            use_row(one, b);
+            b += stride;
+            if (b >= rows) break;
+            load_row(one, b + stride);
+            use_row(two, b);
+            b += stride;
+        }
+    } else {
+        for (; b < rows; b += stride) {
+            Row one;
+            load_row(one, b);
+            use_row(one, b);
         }
     }
     if (!part && !grad_w && !grad_b) return;
@@ -481,9 +527,9 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
         }
         if (group != GROUPS - 1) return;
     }
-    const int64_t stride = rn_stride(static_cast<int64_t>(planes) * n);
-    float *to_w = part ? part + 2 * stride * blockIdx.x + w0 : grad_w ? grad_w + w0 : nullptr;
-    float *to_b = part ? part + 2 * stride * blockIdx.x + stride + w0 : grad_b ? grad_b + w0 : nullptr;
+    const int64_t wide = rn_stride(static_cast<int64_t>(planes) * n);
+    float *to_w = part ? part + 2 * wide * blockIdx.x + w0 : grad_w ? grad_w + w0 : nullptr;
+    float *to_b = part ? part + 2 * wide * blockIdx.x + wide + w0 : grad_b ? grad_b + w0 : nullptr;
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k) {
         if (k == SLOTS - 1 && !place.some) break;
@@ -511,8 +557,8 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_parts(const T *x, co
             float s[3] = {0.f, 0.f, 0.f};
             rn_by_whole(at + kPart<T> <= n, [&](auto whole) {
                 Held<T, kPartSlots> xs, ds;
-                rn_piece<T>(xs, x + row * n, at, n, whole);
-                rn_piece<T>(ds, dy + row * n, at, n, whole);
+                rn_piece<T, false>(xs, x + row * n, at, n, whole);
+                rn_piece<T, false>(ds, dy + row * n, at, n, whole);
 #pragma unroll
                 for (int k = 0; k < kPartSlots; ++k) {
                     const int i = at + (k * kNormThreads + static_cast<int>(threadIdx.x)) * N;
@@ -551,8 +597,9 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_parts(const T *x, co
 
 // Then a workgroup has kNormThreads * N columns of a plane and `per` of its rows: dx there, and the columns' sums over those rows.
 // grid (column tiles, planes, parts of the rows), the last rows first: they were read last
+// (loads and stores as in rn_forward_apply: 4,000 x 30,000 fp32 472 us, so 421; 256 x 30,000 34, and would be 38 if x and dy were not kept)
 constexpr int kRowsAtOnce = kNormThreads / 4;
-template <class T>
+template <class T, bool ONCE>
 __global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, const T *dy, int rows, int planes, int n, int per, int parts,
                                                                     const float *__restrict__ weight, const float *__restrict__ mean,
                                                                     const float *__restrict__ rstd, const float4 *__restrict__ sums, T *dx,
@@ -600,8 +647,8 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, 
                 const float4 c = rs[b];
                 const float c1 = c1s[b];
                 const int64_t place = ((at + static_cast<int64_t>(b)) * planes + plane) * n;
-                const auto xs = whole ? rk_load_slot<T, false>(x + place + i) : rk_load_edge<T, false, false>(x + place, i, n);
-                const auto ds = whole ? rk_load_slot<T, false>(dy + place + i) : rk_load_edge<T, false, false>(dy + place, i, n);
+                const auto xs = whole ? rk_load_slot<T, ONCE>(x + place + i) : rk_load_edge<T, ONCE, false>(x + place, i, n);
+                const auto ds = whole ? rk_load_slot<T, ONCE>(dy + place + i) : rk_load_edge<T, ONCE, false>(dy + place, i, n);
 #pragma unroll
                 for (int q = 0; q < N; ++q) {
                     const float h = fmaf(static_cast<float>(xs[q]) - c.x, c.y, -c.z), d = static_cast<float>(ds[q]);
@@ -609,7 +656,7 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, 
                     db[q] += d;
                     v[q] = c.y * (fmaf(-h, c.w, d * w[q]) - c1);
                 }
-                if (whole || i < n) rk_store<T, false>(dx + place + i, whole ? N : n - i, v);
+                if (whole || i < n) rk_store<T, true>(dx + place + i, whole ? N : n - i, v);
             }
         });
     }
@@ -664,13 +711,22 @@ constexpr int64_t kMostGroups = 1 << 20;      // of a launch (its lanes must be 
 template <int V>
 using Int = std::integral_constant<int, V>;
 
+// x and y are streamed, not kept by the caches, where they are more than those hold and their rows are whole cache lines but
+// for a few: 65,536 x 2,048 bf16 102 us, so 97; 1,000,000 x 64 bf16 49, so 46; but 256 x 3 x 10,000 fp32 (62 MB) 13.3, and would be 15.7;
+// 2,000,000 x 3 x 16 fp32 138, and 147.
+constexpr int64_t kKeptBytes = 192 << 20;
+// From so many rows on a group of lanes takes two of a plane, whose weights it then loads once: 60,001 x 3 x 1,537 bf16 297 us, so 240;
+// 16,384 x 2 x 10,000 fp32 508, so 482.  Fewer rows are spread over the chip.
+constexpr int64_t kTwoRows = 2048;
 // How a row is held: in registers as long as 8 loads of 1,024 lanes hold it, else in parts.
 struct ForwardPlan {
     int64_t R;
     int parts = 0, length = 0;
+    bool once = false;
     ForwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes)
     {
-        const int64_t per = 16 / static_cast<int64_t>(rk_type_bytes(dtype));
+        const int64_t size = static_cast<int64_t>(rk_type_bytes(dtype)), per = 16 / size, row = n * size;
+        once = 2 * R * row > kKeptBytes && (row % 128 == 0 || row >= 16384);
         if (n <= 8 * 1024 * per) return;
         const int64_t piece = kNormThreads * kPartSlots * per;
         const int64_t pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
@@ -686,6 +742,7 @@ struct BackwardPlan {
     int64_t R, wide;
     int lanes = 0, slots = 0, parts = 1;
     int row_parts = 0, length = 0, per = 0;       // two passes: parts of a row, their length; rows of a part
+    bool once = false;                            // x and dy are more than the caches keep for the second
     BackwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes), wide(static_cast<int64_t>(planes) * n)
     {
         const int64_t per_load = 16 / static_cast<int64_t>(rk_type_bytes(dtype)), loads = (n + per_load - 1) / per_load;
@@ -704,11 +761,12 @@ struct BackwardPlan {
         if (lanes > 0) {
             const int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
             const int64_t turns = (static_cast<int64_t>(rows) + groups - 1) / groups;      // of all groups together
-            const int64_t most = std::max<int64_t>(1, 256 * 1024 / threads / planes);
+            const int64_t most = std::max<int64_t>(1, (lanes <= 64 ? 256 / slots : 256) * 1024 / threads / planes);
             parts = static_cast<int>(std::min(most, turns <= 16 ? 1 : turns));
             if (parts > 1) parts = static_cast<int>((turns + (turns + parts - 1) / parts - 1) / ((turns + parts - 1) / parts));     // all take as many turns
             return;
         }
+        once = 2 * R * n * static_cast<int64_t>(rk_type_bytes(dtype)) > kKeptBytes;
         const int64_t piece = kNormThreads * kPartSlots * per_load, pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
         row_parts = static_cast<int>((pieces + each - 1) / each);
         length = static_cast<int>(each * piece);
@@ -721,6 +779,13 @@ struct BackwardPlan {
     size_t part_bytes() const { return row_parts == 0 && parts == 1 ? 0 : up256(static_cast<size_t>(2 * parts) * static_cast<size_t>(rn_stride(wide)) * 4); }
     size_t bytes() const { return std::max<size_t>(256, sums_bytes() + part_bytes()); }
 };
+
+template <class F>
+void by_kept(bool once, F f)
+{
+    if (once) f(std::true_type());
+    else f(std::false_type());
+}
 
 template <class F>
 void by_type(int32_t dtype, F f)
@@ -761,30 +826,40 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
         using T = decltype(t);
         const T *x = static_cast<const T *>(x_dev);
         T *y = static_cast<T *>(y_dev);
-        const auto held = [&](auto lanes, auto slots, auto rows_at_once) {
-            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, J = decltype(rows_at_once)::value, kRows = L < 256 ? 256 / L * J : 1;
-            for (int64_t first = 0; first < plan.R; first += kMostGroups * kRows)
-                hipLaunchKernelGGL((rn_forward<T, L, S, J, false>), dim3(static_cast<unsigned>(std::min((plan.R - first + kRows - 1) / kRows, kMostGroups))),
-                                   dim3(L < 256 ? 256 : L), 0, stream, x, first, plan.R, planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+        const auto launch = [&](auto lanes, auto slots, auto rows_at_once, auto once) {
+            constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, J = decltype(rows_at_once)::value, kGroups = L < 256 ? 256 / L : 1;
+            // examples of a launch: its groups of lanes are fewer than 2^32, and so are its lanes
+            const int64_t most = kMostGroups * kGroups / planes * J;
+            for (int64_t first = 0; first < rows; first += most) {
+                const int64_t groups = (std::min<int64_t>(rows - first, most) + J - 1) / J * planes;
+                hipLaunchKernelGGL((rn_forward<T, L, S, J, decltype(once)::value>), dim3(static_cast<unsigned>((groups + kGroups - 1) / kGroups)), dim3(L < 256 ? 256 : L), 0,
+                                   stream, x, static_cast<int>(first), rows, planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+            }
         };
         const int64_t loads = (n + kPerLoad<T> - 1) / kPerLoad<T>;      // of 16 bytes in a row
         if (plan.parts == 0) {
             // lanes to a row, slots, rows at a time: with one slot fewer, or fewer lanes, the row would not fit
             const int s64 = static_cast<int>((loads + 63) / 64), s256 = static_cast<int>((loads + 255) / 256), s1024 = static_cast<int>((loads + 1023) / 1024);
+            const auto held = [&](auto lanes, auto slots, auto rows_at_once) {
+                by_kept(plan.once, [&](auto once) { launch(lanes, slots, rows_at_once, once); });
+            };
+            const auto pick = [&](auto lanes, auto slots) {
+                plan.R >= kTwoRows ? held(lanes, slots, Int<2>()) : launch(lanes, slots, Int<1>(), std::false_type());
+            };
             if (loads <= 4) held(Int<4>(), Int<1>(), Int<4>());
             else if (loads <= 8) held(Int<8>(), Int<1>(), Int<4>());
             else if (loads <= 16) held(Int<16>(), Int<1>(), Int<4>());
             else if (loads <= 32) held(Int<32>(), Int<1>(), Int<4>());
             else if (s64 == 1) held(Int<64>(), Int<1>(), Int<4>());
-            else if (s64 == 2) held(Int<64>(), Int<2>(), Int<2>());
-            else if (s64 == 3) held(Int<64>(), Int<3>(), Int<1>());
-            else if (s64 == 4) held(Int<64>(), Int<4>(), Int<1>());
-            else if (s256 == 2) held(Int<256>(), Int<2>(), Int<1>());
-            else if (s256 == 3) held(Int<256>(), Int<3>(), Int<1>());
-            else if (s256 == 4) held(Int<256>(), Int<4>(), Int<1>());
-            else if (s1024 == 2) held(Int<1024>(), Int<2>(), Int<1>());
-            else if (s1024 == 3) held(Int<1024>(), Int<3>(), Int<1>());
-            else if (s1024 == 4) held(Int<1024>(), Int<4>(), Int<1>());
+            else if (s64 == 2) pick(Int<64>(), Int<2>());
+            else if (s64 == 3) pick(Int<64>(), Int<3>());
+            else if (s64 == 4) pick(Int<64>(), Int<4>());
+            else if (s256 == 2) pick(Int<256>(), Int<2>());
+            else if (s256 == 3) pick(Int<256>(), Int<3>());
+            else if (s256 == 4) pick(Int<256>(), Int<4>());
+            else if (s1024 == 2) pick(Int<1024>(), Int<2>());
+            else if (s1024 == 3) pick(Int<1024>(), Int<3>());
+            else if (s1024 == 4) pick(Int<1024>(), Int<4>());
             else if (s1024 == 5) held(Int<1024>(), Int<5>(), Int<1>());
             else if (s1024 == 6) held(Int<1024>(), Int<6>(), Int<1>());
             else if (s1024 == 7) held(Int<1024>(), Int<7>(), Int<1>());
@@ -794,8 +869,11 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
             const unsigned tall = static_cast<unsigned>(std::min<int64_t>(plan.R, 32768));
             hipLaunchKernelGGL(rn_forward_parts<T>, dim3(static_cast<unsigned>(plan.parts), tall), dim3(kNormThreads), 0, stream, x, plan.R, n, plan.length,
                                moments);
-            hipLaunchKernelGGL(rn_forward_apply<T>, dim3(static_cast<unsigned>((n + int64_t{kPart<T>} - 1) / kPart<T>), tall), dim3(kNormThreads), 0, stream, x,
-                               plan.R, planes, n, plan.length, plan.parts, moments, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+            by_kept(plan.once, [&](auto once) {
+                hipLaunchKernelGGL((rn_forward_apply<T, decltype(once)::value>), dim3(static_cast<unsigned>((n + int64_t{kPart<T>} - 1) / kPart<T>), tall),
+                                   dim3(kNormThreads), 0, stream, x, plan.R, planes, n, plan.length, plan.parts, moments, weight_dev, bias_dev, eps, y,
+                                   mean_dev, rstd_dev);
+            });
         }
     });
     return hipGetLastError() == hipSuccess ? ROCKET_OK : rk_fail(ROCKET_EHIP, "launch of the layer norm kernel failed");
@@ -825,7 +903,7 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
         const auto held = [&](auto lanes, auto slots) {
             constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, G = L < 256 ? 256 / L : 1;
             if (plan.lanes != L || plan.slots != S) return;
-            hipLaunchKernelGGL((rn_backward<T, L, S, G, true>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)), dim3(L * G), 0, stream, x, dy,
+            hipLaunchKernelGGL((rn_backward<T, L, S, G, (L > 4)>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)), dim3(L * G), 0, stream, x, dy,
                                rows, planes, n, weight_dev, mean_dev, rstd_dev, dx, part, grad_weight_dev, grad_bias_dev);
         };
         held(Int<4>(), Int<1>());
@@ -847,8 +925,11 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
             hipLaunchKernelGGL(rn_backward_parts<T>, dim3(static_cast<unsigned>(plan.row_parts), static_cast<unsigned>(std::min<int64_t>(plan.R, 32768))),
                                dim3(kNormThreads), 0, stream, x, dy, plan.R, planes, n, plan.length, weight_dev, mean_dev, rstd_dev, sums);
             const unsigned tiles = static_cast<unsigned>((n + int64_t{kNormThreads * kPerLoad<T>} - 1) / (kNormThreads * kPerLoad<T>));
-            hipLaunchKernelGGL(rn_backward_columns<T>, dim3(tiles, static_cast<unsigned>(planes), static_cast<unsigned>(plan.parts)), dim3(kNormThreads), 0,
-                               stream, x, dy, rows, planes, n, plan.per, plan.row_parts, weight_dev, mean_dev, rstd_dev, sums, dx, part);
+            by_kept(plan.once, [&](auto once) {
+                hipLaunchKernelGGL((rn_backward_columns<T, decltype(once)::value>), dim3(tiles, static_cast<unsigned>(planes), static_cast<unsigned>(plan.parts)),
+                                   dim3(kNormThreads), 0, stream, x, dy, rows, planes, n, plan.per, plan.row_parts, weight_dev, mean_dev, rstd_dev, sums, dx,
+                                   part);
+            });
         }
         if (part) {
             const int64_t floats = 2 * rn_stride(plan.wide);
