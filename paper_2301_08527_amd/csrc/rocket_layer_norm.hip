@@ -68,7 +68,7 @@ struct Place {
     static constexpr int N = kPerLoad<T>, kStep = LANES * N;
     static constexpr bool kTiny = LANES == 4;
     int n, first, last, skip;      // values of the row; places of slots 0 and SLOTS - 1; values of the last one that do not count
-    bool tiny, some;               // some: the last slot has values that count
+    bool tiny, some, mixed;        // some: the last slot has values that count; mixed: the wavefront has values that do not
     __device__ __forceinline__ Place(int n, int lane) : n(n)
     {
         const int i = lane * N + (SLOTS - 1) * kStep;
@@ -77,6 +77,7 @@ struct Place {
         first = SLOTS > 1 ? lane * N : last;
         skip = min(i - last, N);
         some = tiny ? lane == 0 : skip < N;
+        mixed = __any(tiny || skip > 0);
     }
     __device__ __forceinline__ int at(int k) const { return k < SLOTS - 1 ? first + k * kStep : last; }
     // whether value q of slot k counts
@@ -128,7 +129,8 @@ __device__ __forceinline__ void rn_forget(Held<T, SLOTS> &raw)
     }
 }
 
-// Moments of what LANES lanes hold of a row, `count` values; counts(k, q): whether value q of slot k does.
+// Moments of what LANES lanes hold of a row, `count` values; counts(k, q): whether value q of slot k does.  (Whole slots by a branch of their
+// own: 65,536 x 2,048 bf16 98 us, then 106.)
 template <class T, int LANES, int SLOTS, class F>
 __device__ __forceinline__ Moments rn_moments(const Held<T, SLOTS> &raw, float count, F counts)
 {
@@ -167,11 +169,13 @@ __device__ __forceinline__ Moments rn_join(const Moments &part, float n)
     return {n, shift, rest, rn_lanes_sum<16>(some ? fmaf(part.count * apart, apart, part.m2) : 0.f)};
 }
 
+// The rest of the mean is a rounding or so of x - shift: its product with r loses nothing that counts.
 template <int N>
 __device__ __forceinline__ void rn_normal(const float (&x)[N], const Moments &m, float r, const float (&w)[N], const float (&b)[N], float (&y)[N])
 {
+    const float rest = -m.rest * r;
 #pragma unroll
-    for (int q = 0; q < N; ++q) y[q] = fmaf(((x[q] - m.shift) - m.rest) * r, w[q], b[q]);
+    for (int q = 0; q < N; ++q) y[q] = fmaf(fmaf(x[q] - m.shift, r, rest), w[q], b[q]);
 }
 
 // n as a float: exact up to 2^24, and a rounding of 2^-25 of the mean of squares beyond
@@ -395,7 +399,7 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
                                                               float *__restrict__ part, float *__restrict__ grad_w, float *__restrict__ grad_b)
 {
     constexpr int N = kPerLoad<T>, kWaves = LANES > 64 ? LANES / 64 : 1, kWide = SLOTS * N * LANES;
-    constexpr bool kAhead = sizeof(T) == 2 && SLOTS == 1 && LANES >= 256;       // the next row is loaded before the last one is done with
+    constexpr bool kAhead = sizeof(T) == 2 && SLOTS == 1 && LANES >= 512;       // the next row is loaded before the last one is done with
     static_assert(LANES <= 64 || GROUPS == 1, "a row of several wavefronts has the workgroup to itself");
     __shared__ float meet[2][3][kWaves];
     __shared__ float4 total[GROUPS > 1 ? 2 * kWide / 4 : 1];
@@ -414,6 +418,7 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
     if constexpr (kKeep)
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) load_weights(weight, k, kept[k]);
+    constexpr bool kFloats = sizeof(T) == 4 || SLOTS == 1;     // the slots as floats from the first pass to the second, where there is room for them
     struct Row {
         Held<T, SLOTS> xs, ds;
         float m, r;
@@ -430,18 +435,39 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
         const float m = row.m, r = row.r;
         const float *again = weight;
         if constexpr (!kKeep) asm volatile("" : "+s"(again));       // or the loads are moved out of the loop, into registers that are not there
-        float s[3] = {0.f, 0.f, 0.f};
+        float xf[SLOTS][N], df[SLOTS][N];                           // x - m and dy
+        const auto widen = [&] {
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k)
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    xf[k][q] = static_cast<float>(row.xs[k][q]) - m;
+                    df[k][q] = static_cast<float>(row.ds[k][q]);
+                }
+        };
+        widen();
+        float s[3] = {0.f, 0.f, 0.f};       // of g, g (x - m), x - m
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
             if constexpr (!kKeep) load_weights(again, k, kept[0]);
             const float (&w)[N] = kept[kKeep ? k : 0];
+            if (k == SLOTS - 1 && (LANES == 4 || place.mixed)) {
 #pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const float h = (static_cast<float>(row.xs[k][q]) - m) * r, g = static_cast<float>(row.ds[k][q]) * w[q];
-                const bool count = place.counts(k, q);
-                s[0] += count ? g : 0.f;
-                s[1] += count ? g * h : 0.f;
-                s[2] += count ? h : 0.f;
+                for (int q = 0; q < N; ++q) {
+                    const bool count = place.counts(k, q);
+                    const float g = count ? df[k][q] * w[q] : 0.f, d = count ? xf[k][q] : 0.f;
+                    s[0] += g;
+                    s[1] = fmaf(g, d, s[1]);
+                    s[2] += d;
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    const float g = df[k][q] * w[q];
+                    s[0] += g;
+                    s[1] = fmaf(g, xf[k][q], s[1]);
+                    s[2] += xf[k][q];
+                }
             }
         }
 #pragma unroll
@@ -456,9 +482,13 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
             for (int i = 0; i < 3; ++i) s[i] = rn_lanes_sum<16>(static_cast<int>(threadIdx.x & 15) < kWaves ? meet[turn][i][threadIdx.x & 15] : 0.f);
             turn ^= 1;
         }
-        const float c1 = s[0] * per, e = s[2] * per, c2 = fmaf(-e, s[0], s[1]) * per;
-        rn_forget<T, SLOTS>(row.xs);
-        rn_forget<T, SLOTS>(row.ds);
+        // dx = r (g - c1 - h c2)
+        const float e = s[2] * r * per, c2 = r * fmaf(-e, s[0], s[1] * r) * per, c1 = r * s[0] * per;
+        if constexpr (!kFloats) {
+            rn_forget<T, SLOTS>(row.xs);
+            rn_forget<T, SLOTS>(row.ds);
+            widen();
+        }
         T *to = dx + (b * planes + plane) * n;
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
@@ -467,10 +497,10 @@ __global__ __launch_bounds__(LANES * GROUPS) void rn_backward(const T *x, const 
             float v[N];
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const float h = fmaf(static_cast<float>(row.xs[k][q]) - m, r, -e), d = static_cast<float>(row.ds[k][q]);
-                dw[k][q] = fmaf(d, h, dw[k][q]);
-                db[k][q] += d;
-                v[q] = r * (fmaf(-h, c2, d * w[q]) - c1);
+                const float h = fmaf(xf[k][q], r, -e);
+                dw[k][q] = fmaf(df[k][q], h, dw[k][q]);
+                db[k][q] += df[k][q];
+                v[q] = fmaf(df[k][q] * r, w[q], fmaf(-h, c2, -c1));
             }
             rn_put<T, LANES, SLOTS, STREAM>(to, place, k, v);
         }

@@ -22,7 +22,7 @@
 namespace {
 
 constexpr int kThreads_ = 256;
-// Values of a unit: of the norm and the scaling 16 KB, four loads of a lane (16-bit values in units of 8 KB: 100 million 56 us, so XX);
+// Values of a unit: of the norm and the scaling 16 KB, four loads of a lane (16-bit values in units of 8 KB: 100 million in 56 us, so in 43);
 // of the update as many as there are fp32 parameters in 16 KB.
 constexpr int kUnitBytes = 16384;
 template <class T>
