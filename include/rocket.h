@@ -385,7 +385,8 @@ int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_dev, int32_
 /*
  * Many tensors at once: the global norm of all gradients, clipping, and an update that clips on the way.
  * A list is a host array of `tensors` records; data is device memory (any element's address), count may be 0 (data is then
- * not looked at).  Lists are read during the call only.
+ * not looked at).  Lists are read during the call only.  Tensors that a call writes overlap neither one another nor what it reads,
+ * but for the tensor that they are the new values of (ROCKET_EINVAL).  A list holds at most 2^40 values.
  *
  * rocket_grad_norm: norm = sqrt(sum of the squares of all values of all tensors), and the coefficient that brings a larger
  * norm down to max_norm: norm_dev[0] = norm, norm_dev[1] = norm <= max_norm ? 1 : max_norm / norm (device, 2 doubles).
@@ -393,7 +394,7 @@ int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_dev, int32_
  * order without atomics.  A NaN among the values makes both NaN; an infinity makes the norm infinite and the coefficient 0.
  *
  * rocket_grad_clip: rocket_grad_norm, then out[i] = grads[i] * coefficient, rounded once.  out: a list of the same counts and
- * types (each its own gradient tensor, or overlapping none), or NULL: in place; where the coefficient is 1 nothing is then
+ * types, or NULL: in place; where the coefficient is 1 nothing is then
  * written.
  *
  * rocket_sgd_tensors: out[i] = params[i] - lr * coefficient * grads[i], in fp64, rounded once; params and out are

@@ -13,8 +13,10 @@
 
 #include <algorithm>
 #include <cmath>
+#include <new>
 #include <string>
 #include <type_traits>
+#include <vector>
 
 #include "rocket_elements.hpp"
 #include "rocket_internal.hpp"
@@ -247,6 +249,52 @@ std::string pair_fault(const rocket_tensor *a, const rocket_tensor *b, int32_t t
     return "";
 }
 
+// Whether memory that a call writes (`out`) is written twice or read as something else: every tensor of `out` may be the tensor of
+// `in` that has its place, else it overlaps none of `out`, `in` and `other`.
+bool overlapping(const rocket_tensor *out, const rocket_tensor *in, const rocket_tensor *other, int32_t tensors)
+{
+    struct Span {
+        uintptr_t from, to;
+        bool written;
+    };
+    Span few[3 * kFew];
+    std::vector<Span> many;
+    int32_t k = 0;
+    Span *spans = few;
+    if (tensors > kFew) {
+        many.resize(static_cast<size_t>(tensors) * 3);
+        spans = many.data();
+    }
+    const auto add = [&](const rocket_tensor &t, bool written) {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(t.data);
+        spans[k++] = {from, from + static_cast<uintptr_t>(t.count) * rk_type_bytes(t.dtype), written};
+    };
+    for (int32_t i = 0; i < tensors; ++i) {
+        if (out[i].count == 0) continue;
+        add(out[i], true);
+        if (in[i].data != out[i].data) add(in[i], false);
+        if (other) add(other[i], false);
+    }
+    std::sort(spans, spans + k, [](const Span &a, const Span &b) { return a.from < b.from; });
+    uintptr_t written = 0, read = 0;      // ends of what lies before
+    for (int32_t i = 0; i < k; ++i) {
+        if (spans[i].from < written || (spans[i].written && spans[i].from < read)) return true;
+        uintptr_t &end = spans[i].written ? written : read;
+        end = std::max(end, spans[i].to);
+    }
+    return false;
+}
+
+int check_written(const char *who, const rocket_tensor *out, const rocket_tensor *in, const rocket_tensor *other, int32_t tensors)
+{
+    try {
+        if (overlapping(out, in, other, tensors)) return rk_fail(ROCKET_EINVAL, std::string(who) + ": tensors that are written overlap others");
+    } catch (const std::bad_alloc &) {
+        return rk_fail(ROCKET_ENOMEM, std::string(who) + ": no memory for the list");
+    }
+    return ROCKET_OK;
+}
+
 inline int64_t unit_of(int32_t dtype) { return kUnitBytes / static_cast<int64_t>(rk_type_bytes(dtype)); }
 
 // A list's launches.
@@ -379,6 +427,7 @@ extern "C" int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor 
         if (fault.empty()) fault = pair_fault(grads, out, tensors, true);
         if (!fault.empty()) return rk_fail(ROCKET_EINVAL, std::string(who) + ": out: " + fault);
     }
+    if (const int rc = check_written(who, out ? out : grads, grads, nullptr, tensors); rc != ROCKET_OK) return rc;
     const ListPlan plan(grads, tensors);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     double *partial = static_cast<double *>(ws);
@@ -407,6 +456,7 @@ extern "C" int rocket_sgd_tensors(const rocket_tensor *params, const rocket_tens
     if (fault.empty() && out) fault = pair_fault(grads, out, tensors, false);
     if (!fault.empty()) return rk_fail(ROCKET_EINVAL, who + fault);
     if (!std::isfinite(lr)) return rk_fail(ROCKET_EINVAL, who + "lr must be finite");
+    if (const int rc = check_written("rocket_sgd_tensors", out ? out : params, params, grads, tensors); rc != ROCKET_OK) return rc;
     const ListPlan plan(grads, tensors, kSgdUnit);
     return plan.each<3>({grads, params, out ? out : params}, tensors, [&](const auto &r, int64_t units) {
         by_length(plan.bytes > kKeptBytes, [&](auto once) {

@@ -5,6 +5,7 @@ library.  torch supplies device memory and the current stream.  There is no
 CPU fallback: importing works without a GPU (kernel sampling is host code),
 but the compute calls need the library and a device and fail loudly otherwise.
 """
+import array
 import ctypes as C
 import os
 
@@ -505,19 +506,17 @@ def _type_code(torch, dtype):
     return _TYPE_CODES.get(dtype)
 
 
-def _queue(torch, stream):
-    """The hipStream_t of the call.  (torch.cuda.current_stream makes an object first: 2.6 us of a call's 10.)"""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
-
-
 def _current(torch, stream, *tensors):
-    """Refuses tensors, or a stream, of another device than the current one."""
+    """Refuses tensors, or a stream, of another device than the current one.  Returns the call's hipStream_t."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.device.index != here:
             raise RocketError(ROCKET_EINVAL, "a tensor on %s: the current device is cuda:%d" % (t.device, here))
-    if stream is not None and stream.device.index != here:
+    if stream is None:      # torch.cuda.current_stream makes an object first: 2.6 us of a call's 10
+        return torch._C._cuda_getCurrentRawStream(here)
+    if stream.device.index != here:
         raise RocketError(ROCKET_EINVAL, "a stream of %s: the current device is cuda:%d" % (stream.device, here))
+    return stream.cuda_stream
 
 
 def _empty(torch, shape, dtype, stream):
@@ -534,11 +533,9 @@ def _scratch(torch, need, workspace, stream):
         if need == 0:
             return None, 0, None
         workspace = _empty(torch, need, torch.uint8, stream)
-    elif not (workspace.is_cuda and workspace.is_contiguous()):
-        raise RocketError(ROCKET_EWORKSPACE, "workspace must be a contiguous CUDA tensor")
-    else:
-        _current(torch, stream, workspace)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    elif not (workspace.is_contiguous() and workspace.get_device() == torch.cuda.current_device()):
+        raise RocketError(ROCKET_EWORKSPACE, "workspace must be a contiguous CUDA tensor on the current device")
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def _fits(t, like, dtype, name):
@@ -571,20 +568,22 @@ def rocket_layer_norm(x, weight=None, bias=None, eps=1e-5, planes=1, y=None, mea
     where both are given."""
     import torch
     code, rows, n = _norm_sizes(torch, x, planes)
-    for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is not None:
-            _fits(t, (planes * n,), torch.float32, name)
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        if t is not None:
-            _fits(t, (rows, planes), torch.float32, name)
+    if weight is not None:
+        _fits(weight, (planes * n,), torch.float32, "weight")
+    if bias is not None:
+        _fits(bias, (planes * n,), torch.float32, "bias")
+    if mean is not None:
+        _fits(mean, (rows, planes), torch.float32, "mean")
+    if rstd is not None:
+        _fits(rstd, (rows, planes), torch.float32, "rstd")
     if y is not None:
         _fits(y, x.shape, x.dtype, "y")
-    _current(torch, stream, x, weight, bias, y, mean, rstd)
+    queue = _current(torch, stream, x, weight, bias, y, mean, rstd)
     if y is None:
         y = _empty(torch, x.shape, x.dtype, stream)
     ws, size, keep = _scratch(torch, rocket_layer_norm_workspace_bytes(rows, planes, n, False), workspace, stream)
     _check(load_library().rocket_layer_norm(x.data_ptr(), code, rows, planes, n, _ptr(weight), _ptr(bias), eps, y.data_ptr(),
-                                            _ptr(mean), _ptr(rstd), ws, size, _queue(torch, stream)))
+                                            _ptr(mean), _ptr(rstd), ws, size, queue))
     return y
 
 
@@ -600,10 +599,11 @@ def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, gra
         _fits(weight, (planes * n,), torch.float32, "weight")
     if grad_x is not None:
         _fits(grad_x, x.shape, x.dtype, "grad_x")
-    for t, name in ((grad_weight, "grad_weight"), (grad_bias, "grad_bias")):
-        if t is not None:
-            _fits(t, (planes * n,), torch.float32, name)
-    _current(torch, stream, x, grad_y, mean, rstd, weight, grad_x, grad_weight, grad_bias)
+    if grad_weight is not None:
+        _fits(grad_weight, (planes * n,), torch.float32, "grad_weight")
+    if grad_bias is not None:
+        _fits(grad_bias, (planes * n,), torch.float32, "grad_bias")
+    queue = _current(torch, stream, x, grad_y, mean, rstd, weight, grad_x, grad_weight, grad_bias)
     if grad_x is None:
         grad_x = _empty(torch, x.shape, x.dtype, stream)
     if grad_weight is None:
@@ -614,30 +614,29 @@ def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, gra
     ws, size, keep = _scratch(torch, need, workspace, stream)
     _check(load_library().rocket_layer_norm_backward(
         x.data_ptr(), grad_y.data_ptr(), code, rows, planes, n, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), grad_x.data_ptr(),
-        grad_weight.data_ptr(), grad_bias.data_ptr(), ws, size, _queue(torch, stream)))
+        grad_weight.data_ptr(), grad_bias.data_ptr(), ws, size, queue))
     return grad_x, grad_weight, grad_bias
 
 
 class Tensors:
     """A list of CUDA tensors as the library reads it (rocket_tensor records).  It keeps the tensors alive and holds the
     addresses they have when it is made: make a new one after a tensor's memory was replaced."""
-    _RECORD = np.dtype([("data", np.uint64), ("count", np.int64), ("dtype", np.int32), ("reserved", np.int32)])
 
     def __init__(self, tensors):
         import torch
         self.tensors = list(tensors)
         if not self.tensors:
             raise RocketError(ROCKET_EINVAL, "a list holds one tensor at least")
-        self.device = self.tensors[0].device
-        records = []
+        index = self.tensors[0].get_device()
+        records = array.array("q")          # three words each: address, count, type (and the reserved half)
         for i, t in enumerate(self.tensors):
             code = _type_code(torch, t.dtype)
-            if code is None or not t.is_cuda or not t.is_contiguous() or t.device != self.device:
-                raise RocketError(ROCKET_EINVAL, "tensor %d must be a contiguous float32, bfloat16 or float16 CUDA tensor on %s"
-                                  % (i, self.device))
-            records.append((t.data_ptr(), t.numel(), code, 0))
-        self._records = np.array(records, dtype=self._RECORD)
-        self.address = self._records.ctypes.data
+            if code is None or not t.is_cuda or not t.is_contiguous() or t.get_device() != index:
+                raise RocketError(ROCKET_EINVAL, "tensor %d must be a contiguous float32, bfloat16 or float16 CUDA tensor on one device" % i)
+            records.extend((t.data_ptr(), t.numel(), code))
+        self.device = self.tensors[0].device
+        self._records = records
+        self.address = records.buffer_info()[0]
 
     def __len__(self):
         return len(self.tensors)
@@ -665,11 +664,11 @@ def rocket_grad_norm(grads, max_norm=float("inf"), norm=None, workspace=None, st
     """Returns norm, float64 (2,): the norm over all values of all gradients, and the coefficient min(1, max_norm / norm)."""
     import torch
     grads = rocket_tensors(grads)
-    _current(torch, stream, grads, norm)
+    queue = _current(torch, stream, grads, norm)
     norm = _norm_out(torch, norm, stream)
     need = 0 if workspace is not None else rocket_grad_workspace_bytes(grads)
     ws, size, keep = _scratch(torch, need, workspace, stream)
-    _check(load_library().rocket_grad_norm(grads.address, len(grads), max_norm, norm.data_ptr(), ws, size, _queue(torch, stream)))
+    _check(load_library().rocket_grad_norm(grads.address, len(grads), max_norm, norm.data_ptr(), ws, size, queue))
     return norm
 
 
@@ -686,12 +685,12 @@ def rocket_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, strea
     if out is not None:
         out = rocket_tensors(out)
         _same_length(grads, out)
-    _current(torch, stream, grads, out, norm)
+    queue = _current(torch, stream, grads, out, norm)
     norm = _norm_out(torch, norm, stream)
     need = 0 if workspace is not None else rocket_grad_workspace_bytes(grads)
     ws, size, keep = _scratch(torch, need, workspace, stream)
     _check(load_library().rocket_grad_clip(grads.address, None if out is None else out.address, len(grads), max_norm,
-                                           norm.data_ptr(), ws, size, _queue(torch, stream)))
+                                           norm.data_ptr(), ws, size, queue))
     return norm
 
 
@@ -705,9 +704,9 @@ def rocket_sgd_tensors(params, grads, lr, norm=None, out=None, stream=None):
         _same_length(params, out)
     if norm is not None:
         _fits(norm, (2,), torch.float64, "norm")
-    _current(torch, stream, params, grads, out, norm)
+    queue = _current(torch, stream, params, grads, out, norm)
     _check(load_library().rocket_sgd_tensors(params.address, grads.address, None if out is None else out.address, len(params), lr,
-                                             _ptr(norm), _queue(torch, stream)))
+                                             _ptr(norm), queue))
 
 
 def rocket_sgd_update_clipped(kernels, grad_w, grad_b, lr, norm, recentre=False, stream=None):
@@ -716,9 +715,9 @@ def rocket_sgd_update_clipped(kernels, grad_w, grad_b, lr, norm, recentre=False,
     _fits(grad_w, (kernels.total_weights,), torch.float32, "grad_w")
     _fits(grad_b, (kernels.K,), torch.float32, "grad_b")
     _fits(norm, (2,), torch.float64, "norm")
-    _current(torch, stream, grad_w, grad_b, norm)
+    queue = _current(torch, stream, grad_w, grad_b, norm)
     _check(load_library().rocket_sgd_update_clipped(kernels.handle, grad_w.data_ptr(), grad_b.data_ptr(), lr, int(bool(recentre)),
-                                                    norm.data_ptr(), _queue(torch, stream)))
+                                                    norm.data_ptr(), queue))
 
 
 def _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept):
@@ -743,7 +742,7 @@ def rocket_infer_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, 
     B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept)
     if features is not None:
         _fits(features, (B, p), torch.float32, "features")
-    _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, features)
+    queue = _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, features)
     if features is None:
         features = _empty(torch, (B, p), torch.float32, stream)
     pred = _empty(torch, B, torch.float64, stream)
@@ -751,7 +750,7 @@ def rocket_infer_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, 
     ws, size, keep = _scratch(torch, need, workspace, stream)
     _check(load_library().rocket_infer_normed(
         kernels.handle, x.data_ptr(), int(x.dtype == torch.uint8), B, feature_mask, lam, shift, _ptr(norm_weight), _ptr(norm_bias), eps,
-        coef.data_ptr(), intercept.data_ptr(), features.data_ptr(), pred.data_ptr(), ws, size, _queue(torch, stream)))
+        coef.data_ptr(), intercept.data_ptr(), features.data_ptr(), pred.data_ptr(), ws, size, queue))
     return pred, features
 
 
@@ -772,7 +771,7 @@ def rocket_train_step_normed(kernels, x, feature_mask, norm_weight, norm_bias, c
     if norm_weight is None or norm_bias is None:
         raise RocketError(ROCKET_EINVAL, "norm_weight and norm_bias are trained: both are needed")
     _fits(targets, (B,), torch.float32, "targets")
-    _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, targets, norm)
+    queue = _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, targets, norm)
     norm = _norm_out(torch, norm, stream)
     loss = _empty(torch, 1, torch.float64, stream)
     need = rocket_train_normed_workspace_bytes(kernels, B, feature_mask)
@@ -780,7 +779,7 @@ def rocket_train_step_normed(kernels, x, feature_mask, norm_weight, norm_bias, c
     _check(load_library().rocket_train_step_normed(
         kernels.handle, x.data_ptr(), int(x.dtype == torch.uint8), B, feature_mask, lam, shift, norm_weight.data_ptr(),
         norm_bias.data_ptr(), eps, coef.data_ptr(), intercept.data_ptr(), targets.data_ptr(), lr, int(bool(recentre)), max_norm,
-        loss.data_ptr(), norm.data_ptr(), ws, size, _queue(torch, stream)))
+        loss.data_ptr(), norm.data_ptr(), ws, size, queue))
     return loss, norm
 
 

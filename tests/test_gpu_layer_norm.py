@@ -131,6 +131,18 @@ def test_rows(rows, planes, n, dtype):
     both(rows, planes, n, dtype, seed=rows + n)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n", [100, 500, 700, 1000, 1537, 2001, 2500, 4000, 6001, 9000, 12001, 16384])
+def test_many_rows_of_every_width(n, dtype):
+    """two examples to a group of lanes, the last one alone; rows of whole cache lines beyond what the caches keep"""
+    both(2051, 1, n, dtype, seed=n)
+    both(1027, 2, n, dtype, seed=n + 1)
+
+
+def test_long_rows_beyond_the_caches():
+    both(1501, 1, 40000, "float32", seed=4)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [33, 1001, 2047, 10001, 40001])
 def test_rows_that_start_anywhere(n, dtype):
@@ -282,6 +294,37 @@ def test_same_bits_again_on_a_stream_and_in_a_graph(rows, planes, n, dtype):
         m, r = torch.empty_like(mean), torch.empty_like(rstd)
         want = [rocket.rocket_layer_norm(xs, w, b, planes=planes, mean=m, rstd=r)] + list(rocket.rocket_layer_norm_backward(xs, dy, m, r, w, planes))
         assert all(torch.equal(a, c) for a, c in zip(want, [ys] + out))
+
+
+def test_offsets_beyond_32_bits():
+    """2.25e9 values: 1,000 rows again and again give the same rows again and again"""
+    import torch
+    rows, again, n = 1000, 1100, 2048
+    x, dy, w, b = make(rows, 1, n, "bfloat16", 12)
+    mean, rstd = torch.empty((2, rows, 1), device="cuda")
+    y = rocket.rocket_layer_norm(x, w, b, mean=mean, rstd=rstd)
+    ref = reference(x, w, b, 1, 1e-5, dy)
+    xs, many, mean, rstd = x.repeat(again, 1), dy.repeat(again, 1), mean.repeat(again, 1), rstd.repeat(again, 1)
+    assert xs.numel() > 1 << 31
+    ys = rocket.rocket_layer_norm(xs, w, b)
+    assert bool((ys.view(again, rows, n) == y).all())
+    del ys
+    dx, _, _ = rocket.rocket_layer_norm_backward(x, dy, mean[:rows].contiguous(), rstd[:rows].contiguous(), w)
+    many, dw, db = rocket.rocket_layer_norm_backward(xs, many, mean, rstd, w, grad_x=many)
+    assert bool((many.view(again, rows, n) == dx).all())
+    # every sum is of at most 2,000 rows one after the other, the parts' sums are joined in fp64
+    for got, want, terms in ((dw, ref["dw"], (ref["dy"] * ref["h"]).abs().sum(0)), (db, ref["db"], ref["dy"].abs().sum(0))):
+        bound = again * U * (2000 * terms + (TERMS + 4) * (ref["dy"].abs() * (1 + ref["h"].abs())).sum(0))
+        assert bool(((got.double().view(1, n) - again * want).abs() <= bound).all())
+
+
+def test_more_rows_than_a_launch_holds():
+    import torch
+    rows = (1 << 28) + 5
+    x = torch.arange(rows, device="cuda").remainder_(251).to(torch.bfloat16).view(rows, 1)
+    w, b = torch.tensor([2.0], device="cuda"), torch.tensor([0.5], device="cuda")
+    rocket.rocket_layer_norm(x, w, b, y=x)       # one value is its own mean
+    assert bool((x == 0.5).all())
 
 
 def test_refusals():

@@ -96,6 +96,19 @@ def test_clip_and_update(sizes, kinds, unaligned):
             assert all(torch.equal(p, q) for p, q in zip(params, new))
 
 
+def test_offsets_beyond_32_bits():
+    import torch
+    base = make([1 << 20], ["bfloat16"], 3)[0]
+    big = base.repeat(2100)
+    assert big.numel() > 1 << 31
+    one = exact_norm([base])
+    norm = rocket.rocket_grad_clip([big], 0.5 * one)
+    assert abs(float(norm[0]) / (one * math.sqrt(2100)) - 1) < 1e-9
+    small = [base.clone()]
+    c = float(norm[1])
+    assert bool((big.view(2100, -1) == (small[0].double() * c).to(torch.float32).to(torch.bfloat16)).all())
+
+
 def test_update_without_a_norm():
     import torch
     p, g = make([1000, 33], ["float32"] * 2, 1), make([1000, 33], ["bfloat16", "float32"], 2)

@@ -94,6 +94,33 @@ def test_lists_of_tensors():
     assert lib.rocket_sgd_update_clipped(h.handle, P, P, float("nan"), 0, P, None) == E
 
 
+@pytest.mark.parametrize("more", [0, 300])
+def test_what_is_written_overlaps_nothing(more):
+    """the same tensor twice, one that reaches into the next, results in another's place; addresses that a GPU call would
+    fault on are never reached"""
+    lib = rocket.load_library()
+    rest = [((1 << 30) + 4096 * i, 10, 0) for i in range(more)]
+    rest2 = [((1 << 31) + 4096 * i, 10, 0) for i in range(more)]
+    n = 2 + more
+
+    def clip(grads, out):
+        g, o = _list(*(grads + rest)), None if out is None else _list(*(out + rest2))
+        return lib.rocket_grad_clip(g.ctypes.data, None if o is None else o.ctypes.data, n, 1.0, P, P, BIG, None)
+
+    def sgd(params, grads, out):
+        p, g, o = _list(*(params + rest)), _list(*(grads + rest)), None if out is None else _list(*(out + rest2))
+        return lib.rocket_sgd_tensors(p.ctypes.data, g.ctypes.data, None if o is None else o.ctypes.data, n, 0.1, None, None)
+
+    a, b, c, d = (4096, 100, 0), (8192, 100, 0), (16384, 100, 0), (32768, 100, 0)
+    inside = (4096 + 396, 100, 0)          # begins in a's last value
+    for grads, out in (([a, a], None), ([a, inside], None), ([a, b], [c, c]), ([a, b], [b, a]), ([a, b], [c, inside]), ([a, b], [inside, c]),
+                       ([a, a], [a, c])):
+        assert clip(grads, out) == E and "overlap" in rocket.rocket_last_error(), (grads, out)
+    for params, grads, out in (([a, a], [c, d], None), ([a, b], [a, c], None), ([a, b], [c, inside], None), ([a, b], [c, d], [d, (65536, 100, 0)]),
+                               ([a, b], [c, d], [b, (65536, 100, 0)])):
+        assert sgd(params, grads, out) == E and "overlap" in rocket.rocket_last_error(), (params, grads, out)
+
+
 @pytest.mark.parametrize("tensors", [1, 95, 96, 97, 1000])
 def test_workspace_of_many_tensors(tensors):
     """a partial sum per workgroup: it grows with the values, not with the tensors alone"""
