@@ -3,7 +3,8 @@
 // A row is one plane of one example: R = rows * planes rows of n values, row i has the weights of plane i % planes.
 //   forward   m = mean x, v = mean (x - m)^2, r = 1/sqrt(v + eps), y = (x - m) r w + b
 //   backward  g = dy w, h = (x - m) r:  dx = r (g - mean g - h mean(g h)),  dw = sum dy h,  db = sum dy (over the rows of a plane)
-// Both are bound by memory: some ten operations a value.
+// Both are bound by memory, with some ten vector instructions a value and more; of 16-bit values, where those fill the issue slots at the
+// same time, each counts.
 //
 // The mean that the backward pass is given is rounded to 32 bits, an error of (x - m) that all values of a row share.  With
 // h' = (x - m') r and e = mean h' (0 but for that rounding), h = h' - e: one more sum, and rows whose mean is a million times
@@ -744,11 +745,13 @@ using Int = std::integral_constant<int, V>;
 // x and y are streamed, not kept by the caches, where they are more than those hold and their rows are whole cache lines but
 // for a few: 65,536 x 2,048 bf16 102 us, so 97; 1,000,000 x 64 bf16 49, so 46; but 256 x 3 x 10,000 fp32 (62 MB) 13.3, and would be 15.7;
 // 2,000,000 x 3 x 16 fp32 138, and 147.
-constexpr int64_t kKeptBytes = 192 << 20;
+constexpr double kKeptBytes = 192 << 20;
 // From so many rows on a group of lanes takes two of a plane, whose weights it then loads once: 60,001 x 3 x 1,537 bf16 297 us, so 240;
 // 16,384 x 2 x 10,000 fp32 508, so 482.  Fewer rows are spread over the chip.
 constexpr int64_t kTwoRows = 2048;
-// How a row is held: in registers as long as 8 loads of 1,024 lanes hold it, else in parts.
+// How a row is held: in registers as long as kMostSlots loads of 1,024 lanes hold it, else in parts.  Of more than kFewSlots only if there
+// is a row for each CU: 500 x 125,000 bf16 74.5 us in parts, 57 so; 1,000 x 65,000 fp32 142 and 114; but 64 x 100,000 f16 16 and 19.6.
+constexpr int kMostSlots = 16, kFewSlots = 8, kCus = 256;
 struct ForwardPlan {
     int64_t R;
     int parts = 0, length = 0;
@@ -756,8 +759,8 @@ struct ForwardPlan {
     ForwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes)
     {
         const int64_t size = static_cast<int64_t>(rk_type_bytes(dtype)), per = 16 / size, row = n * size;
-        once = 2 * R * row > kKeptBytes && (row % 128 == 0 || row >= 16384);
-        if (n <= 8 * 1024 * per) return;
+        once = 2.0 * static_cast<double>(R) * static_cast<double>(row) > kKeptBytes && (row % 128 == 0 || row >= 16384);
+        if (n <= (R < kCus ? kFewSlots : kMostSlots) * 1024 * per) return;
         const int64_t piece = kNormThreads * kPartSlots * per;
         const int64_t pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
         parts = static_cast<int>((pieces + each - 1) / each);
@@ -791,12 +794,16 @@ struct BackwardPlan {
         if (lanes > 0) {
             const int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
             const int64_t turns = (static_cast<int64_t>(rows) + groups - 1) / groups;      // of all groups together
+            // a workgroup of 1,024 lanes to a CU, or four of 256; fewer where a wavefront has two slots of each row in flight: 100,000 x 2 x 500
+            // fp32 257 us, so 215
             const int64_t most = std::max<int64_t>(1, (lanes <= 64 ? 256 / slots : 256) * 1024 / threads / planes);
-            parts = static_cast<int>(std::min(most, turns <= 16 ? 1 : turns));
+            // a few turns of one workgroup take less than the second launch (2 x 500 fp32, 32 examples: 10.3 us, with it 12.3; 64: 17.4 and 12.2;
+            // 2 x 10,000, 4 examples: 11 and 13.5, 16: 45 and 13)
+            parts = static_cast<int>(std::min(most, turns <= (lanes <= 64 || slots == 1 ? 8 : 4) ? 1 : turns));
             if (parts > 1) parts = static_cast<int>((turns + (turns + parts - 1) / parts - 1) / ((turns + parts - 1) / parts));     // all take as many turns
             return;
         }
-        once = 2 * R * n * static_cast<int64_t>(rk_type_bytes(dtype)) > kKeptBytes;
+        once = 2.0 * static_cast<double>(R) * n * static_cast<double>(rk_type_bytes(dtype)) > kKeptBytes;
         const int64_t piece = kNormThreads * kPartSlots * per_load, pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
         row_parts = static_cast<int>((pieces + each - 1) / each);
         length = static_cast<int>(each * piece);
@@ -809,6 +816,14 @@ struct BackwardPlan {
     size_t part_bytes() const { return row_parts == 0 && parts == 1 ? 0 : up256(static_cast<size_t>(2 * parts) * static_cast<size_t>(rn_stride(wide)) * 4); }
     size_t bytes() const { return std::max<size_t>(256, sums_bytes() + part_bytes()); }
 };
+
+// f(Int<v>) where v is one of FROM .. TO
+template <int FROM, int TO, class F>
+void by_number(int v, F f)
+{
+    if (v == FROM) f(Int<FROM>());
+    else if constexpr (FROM < TO) by_number<FROM + 1, TO>(v, f);
+}
 
 template <class F>
 void by_kept(bool once, F f)
@@ -881,19 +896,10 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
             else if (loads <= 16) held(Int<16>(), Int<1>(), Int<4>());
             else if (loads <= 32) held(Int<32>(), Int<1>(), Int<4>());
             else if (s64 == 1) held(Int<64>(), Int<1>(), Int<4>());
-            else if (s64 == 2) pick(Int<64>(), Int<2>());
-            else if (s64 == 3) pick(Int<64>(), Int<3>());
-            else if (s64 == 4) pick(Int<64>(), Int<4>());
-            else if (s256 == 2) pick(Int<256>(), Int<2>());
-            else if (s256 == 3) pick(Int<256>(), Int<3>());
-            else if (s256 == 4) pick(Int<256>(), Int<4>());
-            else if (s1024 == 2) pick(Int<1024>(), Int<2>());
-            else if (s1024 == 3) pick(Int<1024>(), Int<3>());
-            else if (s1024 == 4) pick(Int<1024>(), Int<4>());
-            else if (s1024 == 5) held(Int<1024>(), Int<5>(), Int<1>());
-            else if (s1024 == 6) held(Int<1024>(), Int<6>(), Int<1>());
-            else if (s1024 == 7) held(Int<1024>(), Int<7>(), Int<1>());
-            else held(Int<1024>(), Int<8>(), Int<1>());
+            else if (s64 <= 4) by_number<2, 4>(s64, [&](auto slots) { pick(Int<64>(), slots); });
+            else if (s256 <= 4) by_number<2, 4>(s256, [&](auto slots) { pick(Int<256>(), slots); });
+            else if (s1024 <= 4) by_number<2, 4>(s1024, [&](auto slots) { pick(Int<1024>(), slots); });
+            else by_number<5, kMostSlots>(s1024, [&](auto slots) { held(Int<1024>(), slots, Int<1>()); });
         } else {
             float4 *moments = static_cast<float4 *>(ws);
             const unsigned tall = static_cast<unsigned>(std::min<int64_t>(plan.R, 32768));

@@ -139,6 +139,18 @@ def test_many_rows_of_every_width(n, dtype):
     both(1027, 2, n, dtype, seed=n + 1)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+@pytest.mark.parametrize("n", [35000, 40961, 45057, 65535, 65536, 65537, 100001, 131072, 131073])
+def test_a_long_row_for_each_cu(n, dtype):
+    """rows that only then stay in registers"""
+    import torch
+    rows = 259
+    x, _, w, b = make(rows, 1, n, dtype, n)
+    mean, rstd = torch.empty((2, rows, 1), device="cuda")
+    y = rocket.rocket_layer_norm(x, w, b, mean=mean, rstd=rstd)
+    check_forward(y, mean, rstd, reference(x, w, b, 1, 1e-5), dtype, rows, 1)
+
+
 def test_long_rows_beyond_the_caches():
     both(1501, 1, 40000, "float32", seed=4)
 
