@@ -5,7 +5,6 @@ library.  torch supplies device memory and the current stream.  There is no
 CPU fallback: importing works without a GPU (kernel sampling is host code),
 but the compute calls need the library and a device and fail loudly otherwise.
 """
-import array
 import ctypes as C
 import os
 
@@ -627,16 +626,19 @@ class Tensors:
         self.tensors = list(tensors)
         if not self.tensors:
             raise RocketError(ROCKET_EINVAL, "a list holds one tensor at least")
-        index = self.tensors[0].get_device()
-        records = array.array("q")          # three words each: address, count, type (and the reserved half)
-        for i, t in enumerate(self.tensors):
-            code = _type_code(torch, t.dtype)
-            if code is None or not t.is_cuda or not t.is_contiguous() or t.get_device() != index:
-                raise RocketError(ROCKET_EINVAL, "tensor %d must be a contiguous float32, bfloat16 or float16 CUDA tensor on one device" % i)
-            records.extend((t.data_ptr(), t.numel(), code))
-        self.device = self.tensors[0].device
-        self._records = records
-        self.address = records.buffer_info()[0]
+        ts, index = self.tensors, self.tensors[0].get_device()
+        _type_code(torch, torch.float32)
+        codes = [_TYPE_CODES.get(t.dtype) for t in ts]
+        usable = [t.is_cuda and t.is_contiguous() and t.get_device() == index for t in ts]
+        if None in codes or False in usable:
+            i = next(i for i, (c, u) in enumerate(zip(codes, usable)) if c is None or not u)
+            raise RocketError(ROCKET_EINVAL, "tensor %d must be a contiguous float32, bfloat16 or float16 CUDA tensor on one device" % i)
+        self._records = np.empty((len(ts), 3), np.int64)      # address, count, type (and the reserved half)
+        self._records[:, 0] = [t.data_ptr() for t in ts]
+        self._records[:, 1] = [t.numel() for t in ts]
+        self._records[:, 2] = codes
+        self.device = ts[0].device
+        self.address = self._records.ctypes.data
 
     def __len__(self):
         return len(self.tensors)
