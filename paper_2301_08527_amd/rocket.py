@@ -505,13 +505,24 @@ def _type_code(torch, dtype):
     return _TYPE_CODES.get(dtype)
 
 
-def _current(torch, stream, *tensors):
-    """Refuses tensors, or a stream, of another device than the current one.  Returns the call's hipStream_t."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise RocketError(ROCKET_EINVAL, "a tensor on %s: the current device is cuda:%d" % (t.device, here))
-    if stream is None:      # torch.cuda.current_stream makes an object first: 2.6 us of a call's 10
+def _here(torch):
+    """The current device."""
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError) as e:
+        raise RocketError(ROCKET_EHIP, "no GPU visible: these calls have no CPU path") from e
+
+
+def _lists(here, *lists):
+    """Refuses lists on another device than the current one."""
+    for v in lists:
+        if v is not None and v.index != here:
+            raise RocketError(ROCKET_EINVAL, "tensors on cuda:%d: the current device is cuda:%d" % (v.index, here))
+
+
+def _queue(torch, stream, here):
+    """The hipStream_t of a call on device `here`.  (torch.cuda.current_stream makes an object first: 2.6 us of a call's 10.)"""
+    if stream is None:
         return torch._C._cuda_getCurrentRawStream(here)
     if stream.device.index != here:
         raise RocketError(ROCKET_EINVAL, "a stream of %s: the current device is cuda:%d" % (stream.device, here))
@@ -526,31 +537,33 @@ def _empty(torch, shape, dtype, stream):
         return torch.empty(shape, dtype=dtype, device="cuda")
 
 
-def _scratch(torch, need, workspace, stream):
+def _scratch(torch, need, workspace, stream, here):
     """(address, bytes) of the workspace, and the tensor to keep until the call was made."""
     if workspace is None:
         if need == 0:
             return None, 0, None
         workspace = _empty(torch, need, torch.uint8, stream)
-    elif not (workspace.is_contiguous() and workspace.get_device() == torch.cuda.current_device()):
+    elif not (workspace.get_device() == here and workspace.is_contiguous()):
         raise RocketError(ROCKET_EWORKSPACE, "workspace must be a contiguous CUDA tensor on the current device")
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
-def _fits(t, like, dtype, name):
-    """An output or input that has to have a shape and a type."""
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == like):
-        raise RocketError(ROCKET_EINVAL, "%s must be a contiguous %s CUDA tensor of shape %s" % (name, dtype, tuple(like)))
+def _fits(t, like, dtype, name, here):
+    """An output or input that has to have a shape, a type and the current device."""
+    if not (t.get_device() == here and t.dtype is dtype and t.is_contiguous() and t.shape == like):
+        raise RocketError(ROCKET_EINVAL, "%s must be a contiguous %s tensor of shape %s on the current device, cuda:%d"
+                          % (name, dtype, tuple(like), here))
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _norm_sizes(torch, x, planes):
+def _norm_sizes(torch, x, planes, here):
     code = _type_code(torch, x.dtype)
-    if not (x.is_cuda and code is not None and x.is_contiguous() and x.dim() == 2):
-        raise RocketError(ROCKET_EINVAL, "x must be a contiguous float32, bfloat16 or float16 CUDA tensor (rows, planes * n)")
+    if not (code is not None and x.get_device() == here and x.is_contiguous() and x.dim() == 2):
+        raise RocketError(ROCKET_EINVAL, "x must be a contiguous float32, bfloat16 or float16 tensor (rows, planes * n) on the current "
+                          "device, cuda:%d" % here)
     rows, wide = x.shape
     if planes < 1 or rows < 1 or wide < 1 or wide % planes:
         raise RocketError(ROCKET_ESHAPE, "x (%d, %d) is not rows of %d planes" % (rows, wide, planes))
@@ -566,21 +579,22 @@ def rocket_layer_norm(x, weight=None, bias=None, eps=1e-5, planes=1, y=None, mea
     normalised by itself.  Returns y (x's type); mean and rstd, float32 (rows, planes), are written for the backward pass
     where both are given."""
     import torch
-    code, rows, n = _norm_sizes(torch, x, planes)
+    here = _here(torch)
+    code, rows, n = _norm_sizes(torch, x, planes, here)
     if weight is not None:
-        _fits(weight, (planes * n,), torch.float32, "weight")
+        _fits(weight, (planes * n,), torch.float32, "weight", here)
     if bias is not None:
-        _fits(bias, (planes * n,), torch.float32, "bias")
+        _fits(bias, (planes * n,), torch.float32, "bias", here)
     if mean is not None:
-        _fits(mean, (rows, planes), torch.float32, "mean")
+        _fits(mean, (rows, planes), torch.float32, "mean", here)
     if rstd is not None:
-        _fits(rstd, (rows, planes), torch.float32, "rstd")
+        _fits(rstd, (rows, planes), torch.float32, "rstd", here)
     if y is not None:
-        _fits(y, x.shape, x.dtype, "y")
-    queue = _current(torch, stream, x, weight, bias, y, mean, rstd)
+        _fits(y, x.shape, x.dtype, "y", here)
+    queue = _queue(torch, stream, here)
     if y is None:
         y = _empty(torch, x.shape, x.dtype, stream)
-    ws, size, keep = _scratch(torch, rocket_layer_norm_workspace_bytes(rows, planes, n, False), workspace, stream)
+    ws, size, keep = _scratch(torch, rocket_layer_norm_workspace_bytes(rows, planes, n, False), workspace, stream, here)
     _check(load_library().rocket_layer_norm(x.data_ptr(), code, rows, planes, n, _ptr(weight), _ptr(bias), eps, y.data_ptr(),
                                             _ptr(mean), _ptr(rstd), ws, size, queue))
     return y
@@ -590,19 +604,20 @@ def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, gra
                                workspace=None, stream=None):
     """Returns (grad_x of x's type, grad_weight, grad_bias float32 (planes * n,)).  grad_x may be grad_y."""
     import torch
-    code, rows, n = _norm_sizes(torch, x, planes)
-    _fits(grad_y, x.shape, x.dtype, "grad_y")
-    _fits(mean, (rows, planes), torch.float32, "mean")
-    _fits(rstd, (rows, planes), torch.float32, "rstd")
+    here = _here(torch)
+    code, rows, n = _norm_sizes(torch, x, planes, here)
+    _fits(grad_y, x.shape, x.dtype, "grad_y", here)
+    _fits(mean, (rows, planes), torch.float32, "mean", here)
+    _fits(rstd, (rows, planes), torch.float32, "rstd", here)
     if weight is not None:
-        _fits(weight, (planes * n,), torch.float32, "weight")
+        _fits(weight, (planes * n,), torch.float32, "weight", here)
     if grad_x is not None:
-        _fits(grad_x, x.shape, x.dtype, "grad_x")
+        _fits(grad_x, x.shape, x.dtype, "grad_x", here)
     if grad_weight is not None:
-        _fits(grad_weight, (planes * n,), torch.float32, "grad_weight")
+        _fits(grad_weight, (planes * n,), torch.float32, "grad_weight", here)
     if grad_bias is not None:
-        _fits(grad_bias, (planes * n,), torch.float32, "grad_bias")
-    queue = _current(torch, stream, x, grad_y, mean, rstd, weight, grad_x, grad_weight, grad_bias)
+        _fits(grad_bias, (planes * n,), torch.float32, "grad_bias", here)
+    queue = _queue(torch, stream, here)
     if grad_x is None:
         grad_x = _empty(torch, x.shape, x.dtype, stream)
     if grad_weight is None:
@@ -610,7 +625,7 @@ def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, gra
     if grad_bias is None:
         grad_bias = _empty(torch, (planes * n,), torch.float32, stream)
     need = 0 if workspace is not None else rocket_layer_norm_workspace_bytes(rows, planes, n, True)
-    ws, size, keep = _scratch(torch, need, workspace, stream)
+    ws, size, keep = _scratch(torch, need, workspace, stream, here)
     _check(load_library().rocket_layer_norm_backward(
         x.data_ptr(), grad_y.data_ptr(), code, rows, planes, n, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), grad_x.data_ptr(),
         grad_weight.data_ptr(), grad_bias.data_ptr(), ws, size, queue))
@@ -637,7 +652,7 @@ class Tensors:
         self._records[:, 0] = [t.data_ptr() for t in ts]
         self._records[:, 1] = [t.numel() for t in ts]
         self._records[:, 2] = codes
-        self.device = ts[0].device
+        self.index = index
         self.address = self._records.ctypes.data
 
     def __len__(self):
@@ -655,21 +670,22 @@ def rocket_grad_workspace_bytes(grads):
     return int(load_library().rocket_grad_workspace_bytes(grads.address, len(grads)))
 
 
-def _norm_out(torch, norm, stream):
+def _norm_out(torch, norm, stream, here):
     if norm is None:
         return _empty(torch, 2, torch.float64, stream)
-    _fits(norm, (2,), torch.float64, "norm")
+    _fits(norm, (2,), torch.float64, "norm", here)
     return norm
 
 
 def rocket_grad_norm(grads, max_norm=float("inf"), norm=None, workspace=None, stream=None):
     """Returns norm, float64 (2,): the norm over all values of all gradients, and the coefficient min(1, max_norm / norm)."""
     import torch
-    grads = rocket_tensors(grads)
-    queue = _current(torch, stream, grads, norm)
-    norm = _norm_out(torch, norm, stream)
+    grads, here = rocket_tensors(grads), _here(torch)
+    _lists(here, grads)
+    queue = _queue(torch, stream, here)
+    norm = _norm_out(torch, norm, stream, here)
     need = 0 if workspace is not None else rocket_grad_workspace_bytes(grads)
-    ws, size, keep = _scratch(torch, need, workspace, stream)
+    ws, size, keep = _scratch(torch, need, workspace, stream, here)
     _check(load_library().rocket_grad_norm(grads.address, len(grads), max_norm, norm.data_ptr(), ws, size, queue))
     return norm
 
@@ -683,14 +699,15 @@ def rocket_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, strea
     """Scales the gradients (in place, or into `out`) so that their norm is at most max_norm.  Returns norm as
     rocket_grad_norm does."""
     import torch
-    grads = rocket_tensors(grads)
+    grads, here = rocket_tensors(grads), _here(torch)
     if out is not None:
         out = rocket_tensors(out)
         _same_length(grads, out)
-    queue = _current(torch, stream, grads, out, norm)
-    norm = _norm_out(torch, norm, stream)
+    _lists(here, grads, out)
+    queue = _queue(torch, stream, here)
+    norm = _norm_out(torch, norm, stream, here)
     need = 0 if workspace is not None else rocket_grad_workspace_bytes(grads)
-    ws, size, keep = _scratch(torch, need, workspace, stream)
+    ws, size, keep = _scratch(torch, need, workspace, stream, here)
     _check(load_library().rocket_grad_clip(grads.address, None if out is None else out.address, len(grads), max_norm,
                                            norm.data_ptr(), ws, size, queue))
     return norm
@@ -699,14 +716,15 @@ def rocket_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, strea
 def rocket_sgd_tensors(params, grads, lr, norm=None, out=None, stream=None):
     """params (or `out`) = params - lr * norm[1] * grads; norm as rocket_grad_norm returns it, or None: not clipped."""
     import torch
-    params, grads = rocket_tensors(params), rocket_tensors(grads)
+    params, grads, here = rocket_tensors(params), rocket_tensors(grads), _here(torch)
     _same_length(params, grads)
     if out is not None:
         out = rocket_tensors(out)
         _same_length(params, out)
+    _lists(here, params, grads, out)
     if norm is not None:
-        _fits(norm, (2,), torch.float64, "norm")
-    queue = _current(torch, stream, params, grads, out, norm)
+        _fits(norm, (2,), torch.float64, "norm", here)
+    queue = _queue(torch, stream, here)
     _check(load_library().rocket_sgd_tensors(params.address, grads.address, None if out is None else out.address, len(params), lr,
                                              _ptr(norm), queue))
 
@@ -714,25 +732,26 @@ def rocket_sgd_tensors(params, grads, lr, norm=None, out=None, stream=None):
 def rocket_sgd_update_clipped(kernels, grad_w, grad_b, lr, norm, recentre=False, stream=None):
     """rocket_sgd_update with lr * norm[1]; norm as rocket_grad_norm returns it."""
     import torch
-    _fits(grad_w, (kernels.total_weights,), torch.float32, "grad_w")
-    _fits(grad_b, (kernels.K,), torch.float32, "grad_b")
-    _fits(norm, (2,), torch.float64, "norm")
-    queue = _current(torch, stream, grad_w, grad_b, norm)
+    here = _here(torch)
+    _fits(grad_w, (kernels.total_weights,), torch.float32, "grad_w", here)
+    _fits(grad_b, (kernels.K,), torch.float32, "grad_b", here)
+    _fits(norm, (2,), torch.float64, "norm", here)
+    queue = _queue(torch, stream, here)
     _check(load_library().rocket_sgd_update_clipped(kernels.handle, grad_w.data_ptr(), grad_b.data_ptr(), lr, int(bool(recentre)),
                                                     norm.data_ptr(), queue))
 
 
-def _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept):
-    if not (x.is_cuda and x.dtype in (torch.float32, torch.uint8) and x.is_contiguous() and x.dim() == 3):
-        raise RocketError(ROCKET_EINVAL, "x must be a contiguous float32 or uint8 CUDA tensor of shape (B, C, L)")
+def _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, here):
+    if not (x.get_device() == here and x.dtype in (torch.float32, torch.uint8) and x.is_contiguous() and x.dim() == 3):
+        raise RocketError(ROCKET_EINVAL, "x must be a contiguous float32 or uint8 tensor of shape (B, C, L) on the current device, cuda:%d" % here)
     if x.shape[1] != kernels.C or x.shape[2] != kernels.L:
         raise RocketError(ROCKET_ESHAPE, "x does not match the kernels' (C, L)")
     p = rocket_num_features(feature_mask) * kernels.K
     for t, name in ((norm_weight, "norm_weight"), (norm_bias, "norm_bias")):
         if t is not None:
-            _fits(t, (p,), torch.float32, name)
-    _fits(coef, (p,), torch.float64, "coef")
-    _fits(intercept, (1,), torch.float64, "intercept")
+            _fits(t, (p,), torch.float32, name, here)
+    _fits(coef, (p,), torch.float64, "coef", here)
+    _fits(intercept, (1,), torch.float64, "intercept", here)
     return x.shape[0], p
 
 
@@ -741,15 +760,16 @@ def rocket_infer_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, 
     """rocket_infer with a layer norm of every feature plane before the head.  norm_weight, norm_bias: float32 (F*K,) or
     None.  Returns (pred float64 (B,), the normalised features float32 (B, F*K))."""
     import torch
-    B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept)
+    here = _here(torch)
+    B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, here)
     if features is not None:
-        _fits(features, (B, p), torch.float32, "features")
-    queue = _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, features)
+        _fits(features, (B, p), torch.float32, "features", here)
+    queue = _queue(torch, stream, here)
     if features is None:
         features = _empty(torch, (B, p), torch.float32, stream)
     pred = _empty(torch, B, torch.float64, stream)
     need = int(load_library().rocket_infer_normed_workspace_bytes(kernels.handle, B, feature_mask))
-    ws, size, keep = _scratch(torch, need, workspace, stream)
+    ws, size, keep = _scratch(torch, need, workspace, stream, here)
     _check(load_library().rocket_infer_normed(
         kernels.handle, x.data_ptr(), int(x.dtype == torch.uint8), B, feature_mask, lam, shift, _ptr(norm_weight), _ptr(norm_bias), eps,
         coef.data_ptr(), intercept.data_ptr(), features.data_ptr(), pred.data_ptr(), ws, size, queue))
@@ -769,15 +789,16 @@ def rocket_train_step_normed(kernels, x, feature_mask, norm_weight, norm_bias, c
     """One clipped gradient-descent step on the kernels and, in place, on norm_weight and norm_bias (float32 (F*K,)).
     Returns (loss before the update, float64 (1,), norm as rocket_grad_norm returns it)."""
     import torch
-    B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept)
+    here = _here(torch)
+    B, p = _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, here)
     if norm_weight is None or norm_bias is None:
         raise RocketError(ROCKET_EINVAL, "norm_weight and norm_bias are trained: both are needed")
-    _fits(targets, (B,), torch.float32, "targets")
-    queue = _current(torch, stream, x, norm_weight, norm_bias, coef, intercept, targets, norm)
-    norm = _norm_out(torch, norm, stream)
+    _fits(targets, (B,), torch.float32, "targets", here)
+    queue = _queue(torch, stream, here)
+    norm = _norm_out(torch, norm, stream, here)
     loss = _empty(torch, 1, torch.float64, stream)
     need = rocket_train_normed_workspace_bytes(kernels, B, feature_mask)
-    ws, size, keep = _scratch(torch, need, workspace, stream)
+    ws, size, keep = _scratch(torch, need, workspace, stream, here)
     _check(load_library().rocket_train_step_normed(
         kernels.handle, x.data_ptr(), int(x.dtype == torch.uint8), B, feature_mask, lam, shift, norm_weight.data_ptr(),
         norm_bias.data_ptr(), eps, coef.data_ptr(), intercept.data_ptr(), targets.data_ptr(), lr, int(bool(recentre)), max_norm,
