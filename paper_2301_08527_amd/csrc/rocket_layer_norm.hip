@@ -769,13 +769,17 @@ struct ForwardPlan {
     size_t bytes() const { return up256(static_cast<size_t>(R) * static_cast<size_t>(parts) * sizeof(float4)); }
 };
 
+// One pass of the backward pass streams x, dy and dx where they are more than this: 677 x 2 x 10,000 fp32 (162 MB) 43 us, so 40.5, 65,536 x 2,048
+// bf16 159 and 149, but 400 x 10,000 fp32 (48 MB) 19.6, and would be 22, 5,000 x 1,000 18.3 and 20.5.
+constexpr double kHeldKeptBytes = 128 << 20;
+
 // The backward pass.  `lanes` x `slots` hold a row (0: rows are too long and go in two passes); the rows of a plane are dealt out
 // to `parts` workgroups.
 struct BackwardPlan {
     int64_t R, wide;
     int lanes = 0, slots = 0, parts = 1;
     int row_parts = 0, length = 0, per = 0;       // two passes: parts of a row, their length; rows of a part
-    bool once = false;                            // x and dy are more than the caches keep for the second
+    bool once = false;                            // nothing is kept by the caches; of two passes: for the second
     BackwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes), wide(static_cast<int64_t>(planes) * n)
     {
         const int64_t per_load = 16 / static_cast<int64_t>(rk_type_bytes(dtype)), loads = (n + per_load - 1) / per_load;
@@ -791,7 +795,9 @@ struct BackwardPlan {
         else if (loads <= 1024) take(1024, 1);
         else if (loads <= 2048) take(1024, 2);
         else if (loads <= 5 * 1024 && dtype == ROCKET_F32) take(1024, static_cast<int>((loads + 1023) / 1024));
+        const double bytes = static_cast<double>(R) * n * static_cast<double>(rk_type_bytes(dtype));
         if (lanes > 0) {
+            once = 3.0 * bytes > kHeldKeptBytes;
             const int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes < 256 ? 256 : lanes;
             const int64_t turns = (static_cast<int64_t>(rows) + groups - 1) / groups;      // of all groups together
             // a workgroup of 1,024 lanes to a CU, or four of 256; fewer where a wavefront has two slots of each row in flight: 100,000 x 2 x 500
@@ -803,7 +809,7 @@ struct BackwardPlan {
             if (parts > 1) parts = static_cast<int>((turns + (turns + parts - 1) / parts - 1) / ((turns + parts - 1) / parts));     // all take as many turns
             return;
         }
-        once = 2.0 * static_cast<double>(R) * n * static_cast<double>(rk_type_bytes(dtype)) > kKeptBytes;
+        once = 2.0 * bytes > kKeptBytes;
         const int64_t piece = kNormThreads * kPartSlots * per_load, pieces = (n + piece - 1) / piece, each = (pieces + kMostParts - 1) / kMostParts;
         row_parts = static_cast<int>((pieces + each - 1) / each);
         length = static_cast<int>(each * piece);
@@ -939,8 +945,10 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
         const auto held = [&](auto lanes, auto slots) {
             constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, G = L < 256 ? 256 / L : 1;
             if (plan.lanes != L || plan.slots != S) return;
-            hipLaunchKernelGGL((rn_backward<T, L, S, G, (L > 4)>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)), dim3(L * G), 0, stream, x, dy,
-                               rows, planes, n, weight_dev, mean_dev, rstd_dev, dx, part, grad_weight_dev, grad_bias_dev);
+            by_kept(plan.once && L > 4, [&](auto once) {
+                hipLaunchKernelGGL((rn_backward<T, L, S, G, decltype(once)::value>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)),
+                                   dim3(L * G), 0, stream, x, dy, rows, planes, n, weight_dev, mean_dev, rstd_dev, dx, part, grad_weight_dev, grad_bias_dev);
+            });
         };
         held(Int<4>(), Int<1>());
         held(Int<8>(), Int<1>());
