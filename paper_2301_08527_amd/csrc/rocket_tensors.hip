@@ -7,6 +7,7 @@
 //   rt_squares   sums of squares, fp64: a partial sum per workgroup
 //   rt_finish    norm = sqrt(sum of the partial sums), coefficient = norm <= max ? 1 : max / norm
 //   rt_scale     out = grad * coefficient
+//   rt_few       all of these, for a list that one workgroup goes through sooner than two launches do
 //   rt_sgd       out = param - lr * coefficient * grad
 // All are bound by memory.
 #include <hip/hip_runtime.h>
@@ -32,6 +33,10 @@ constexpr int kUnit = kUnitBytes / static_cast<int>(sizeof(T));
 constexpr int kSgdUnit = kUnit<float>;
 constexpr int kMostSums = 2048;           // workgroups of all rt_squares over a list together, eight to a CU
 constexpr int kMostGroups = 1 << 20;      // of another launch (its lanes must be fewer than 2^32)
+// A list of so few units is one workgroup's: rt_few goes through 16 of them in the time of rt_squares, and no rt_finish follows (norm and
+// update of 48,000 values 18.4 us, so 14.6).  Scaling them too it beats a launch for that up to 6 (8,000 values 13.3 us, so 9.0; 64,000 would
+// be 14.5 against 12.6).
+constexpr int kFewUnits = 16, kFewScaled = 6;
 constexpr int kJoinedSums = 1024;         // partial sums up to which every workgroup of rt_scale adds them up itself: no rt_finish
 
 // Tensors of a launch, with POINTERS addresses each: a few, or as many as the arguments may hold.
@@ -62,13 +67,18 @@ __device__ __forceinline__ int tensor_of(const Records<P, M> &r, int u)
     return __builtin_amdgcn_readfirstlane(found - 1);
 }
 
-// f(type, whole, tensor, first value, values) for the units of this workgroup.  UNIT: values of a unit, 0: kUnit of the type
+// Which units kThreads_ lanes work on, first, first + stride, ...: those of a workgroup by default.
+struct Turn {
+    int first = static_cast<int>(blockIdx.x), stride = static_cast<int>(gridDim.x), lane = static_cast<int>(threadIdx.x);
+};
+
+// f(type, whole, tensor, first value, values) for these units.  UNIT: values of a unit, 0: kUnit of the type
 template <int UNIT, int P, int M, class F>
-__device__ __forceinline__ void each_unit(const Records<P, M> &r, F f)
+__device__ __forceinline__ void each_unit(const Records<P, M> &r, const Turn &turn, F f)
 {
     const int units = r.first[r.tensors];
     int t = 0, begin = 0, end = 0;
-    for (int u = static_cast<int>(blockIdx.x); u < units; u += static_cast<int>(gridDim.x)) {
+    for (int u = turn.first; u < units; u += turn.stride) {
         if (u < begin || u >= end) {
             t = tensor_of(r, u);
             begin = r.first[t];
@@ -86,13 +96,14 @@ __device__ __forceinline__ void each_unit(const Records<P, M> &r, F f)
     }
 }
 
+template <int THREADS = kThreads_>
 __device__ __forceinline__ double group_sum(double v, double *lds)
 {
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.0;
-    for (int w = 0; w < kThreads_ / 64; ++w) v += lds[w];
+    for (int w = 0; w < THREADS / 64; ++w) v += lds[w];
     return v;
 }
 
@@ -107,15 +118,14 @@ __device__ __forceinline__ void load_unit(const T *p, int i, int step, int value
 
 // STREAM: the list is too long for the caches to keep until the next pass over it
 template <bool STREAM, class R>
-__global__ __launch_bounds__(kThreads_) void rt_squares(const R r, double *__restrict__ partial)
+__device__ __forceinline__ double squares_of(const R &r, const Turn &turn)
 {
-    __shared__ double lds[kThreads_ / 64];
     double s = 0.0;
-    each_unit<0>(r, [&](auto type, auto whole, int t, int64_t at, int values) {
+    each_unit<0>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
         constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
         const T *g = static_cast<const T *>(r.data[0][t]) + at;
-        const int i = static_cast<int>(threadIdx.x) * N;
+        const int i = turn.lane * N;
         typename RkSlot<T>::V v[kLoads];
         load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
 #pragma unroll
@@ -126,18 +136,31 @@ __global__ __launch_bounds__(kThreads_) void rt_squares(const R r, double *__res
                 s = fma(d, d, s);
             }
     });
-    s = group_sum(s, lds);
+    return s;
+}
+
+template <bool STREAM, class R>
+__global__ __launch_bounds__(kThreads_) void rt_squares(const R r, double *__restrict__ partial)
+{
+    __shared__ double lds[kThreads_ / 64];
+    const double s = group_sum(squares_of<STREAM>(r, Turn()), lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-// {norm, coefficient} from the partial sums, in a fixed order
+// {norm, coefficient}
+__device__ __forceinline__ double2 norm_and_coefficient(double squares, double max_norm)
+{
+    const double norm = sqrt(squares);
+    return make_double2(norm, norm <= max_norm ? 1.0 : max_norm / norm);       // NaN stays NaN
+}
+
+// from the partial sums, in a fixed order
 __device__ __forceinline__ double2 norm_of(const double *partial, int count, double max_norm, double *lds)
 {
     double s = 0.0;
 #pragma unroll 8
     for (int i = threadIdx.x; i < count; i += kThreads_) s += partial[i];
-    const double norm = sqrt(group_sum(s, lds));
-    return make_double2(norm, norm <= max_norm ? 1.0 : max_norm / norm);       // NaN stays NaN
+    return norm_and_coefficient(group_sum(s, lds), max_norm);
 }
 
 __global__ __launch_bounds__(kThreads_) void rt_finish(const double *__restrict__ partial, int count, double max_norm, double *__restrict__ out)
@@ -150,8 +173,30 @@ __global__ __launch_bounds__(kThreads_) void rt_finish(const double *__restrict_
     }
 }
 
-// r.data: gradients, results.  count > 0: the norm is still in `count` partial sums, which every workgroup adds up; workgroup 0
-// writes it.
+// r.data: gradients, results
+template <bool STREAM, class R>
+__device__ __forceinline__ void scale_units(const R &r, const Turn &turn, double c)
+{
+    each_unit<0>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
+        using T = decltype(type);
+        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
+        const T *g = static_cast<const T *>(r.data[0][t]) + at;
+        T *o = static_cast<T *>(r.data[1][t]) + at;
+        const int i = turn.lane * N;
+        typename RkSlot<T>::V v[kLoads];
+        load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            // the product in fp64: the coefficient of a norm beyond 1e38 would lose its digits in fp32
+            float u[N];
+#pragma unroll
+            for (int q = 0; q < N; ++q) u[q] = static_cast<float>(static_cast<double>(static_cast<float>(v[k][q])) * c);
+            rk_store<T, true>(o + i + k * kStep, whole ? N : values - i - k * kStep, u);
+        }
+    });
+}
+
+// count > 0: the norm is still in `count` partial sums, which every workgroup adds up; workgroup 0 writes it.
 template <bool STREAM, class R>
 __global__ __launch_bounds__(kThreads_) void rt_scale(const R r, const double *__restrict__ partial, int count, double max_norm, double *__restrict__ norm,
                                                       int in_place)
@@ -169,23 +214,27 @@ __global__ __launch_bounds__(kThreads_) void rt_scale(const R r, const double *_
         c = norm[1];
     }
     if (in_place && c == 1.0) return;
-    each_unit<0>(r, [&](auto type, auto whole, int t, int64_t at, int values) {
-        using T = decltype(type);
-        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
-        const T *g = static_cast<const T *>(r.data[0][t]) + at;
-        T *o = static_cast<T *>(r.data[1][t]) + at;
-        const int i = static_cast<int>(threadIdx.x) * N;
-        typename RkSlot<T>::V v[kLoads];
-        load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            // the product in fp64: the coefficient of a norm beyond 1e38 would lose its digits in fp32
-            float u[N];
-#pragma unroll
-            for (int q = 0; q < N; ++q) u[q] = static_cast<float>(static_cast<double>(static_cast<float>(v[k][q])) * c);
-            rk_store<T, true>(o + i + k * kStep, whole ? N : values - i - k * kStep, u);
-        }
-    });
+    scale_units<STREAM>(r, Turn(), c);
+}
+
+// A list of few units by one workgroup of kQuarters times kThreads_ lanes: the norm and, SCALE, the scaling too (every square was
+// added before the first value is written).
+constexpr int kQuarters = 4;
+template <bool SCALE, class R>
+__global__ __launch_bounds__(kQuarters * kThreads_) void rt_few(const R r, double max_norm, double *__restrict__ norm, int in_place)
+{
+    __shared__ double lds[kQuarters * kThreads_ / 64];
+    Turn turn;
+    turn.first = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kThreads_);
+    turn.stride = kQuarters;
+    turn.lane = static_cast<int>(threadIdx.x) % kThreads_;
+    const double2 n = norm_and_coefficient(group_sum<kQuarters * kThreads_>(squares_of<false>(r, turn), lds), max_norm);
+    if (threadIdx.x == 0) {
+        norm[0] = n.x;
+        norm[1] = n.y;
+    }
+    if constexpr (SCALE)
+        if (!in_place || n.y != 1.0) scale_units<false>(r, turn, n.y);
 }
 
 // r.data: gradients, parameters, results
@@ -193,13 +242,14 @@ template <bool STREAM, class R>
 __global__ __launch_bounds__(kThreads_) void rt_sgd(const R r, double lr, const double *__restrict__ norm)
 {
     const double rate = norm ? lr * norm[1] : lr;
-    each_unit<kSgdUnit>(r, [&](auto type, auto whole, int t, int64_t at, int values) {
+    const Turn turn;
+    each_unit<kSgdUnit>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
         constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kSgdUnit / kStep;
         const T *g = static_cast<const T *>(r.data[0][t]) + at;
         const float *p = static_cast<const float *>(r.data[1][t]) + at;
         float *o = static_cast<float *>(r.data[2][t]) + at;
-        const int i = static_cast<int>(threadIdx.x) * N;
+        const int i = turn.lane * N;
         typename RkSlot<T>::V v[kLoads];
         RkSlot<float>::V w[kLoads * N / 4];
         load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
@@ -340,6 +390,7 @@ struct ListPlan {
         }
         return ROCKET_OK;
     }
+    bool few() const { return units > 0 && units <= kFewUnits; }       // one launch: no tensor without a unit is in it
     // partial sums of a launch of a norm: of kMostSums as many as it has of the units
     int64_t sums(int64_t some) const { return std::min(some, std::max<int64_t>(1, kMostSums * some / units)); }
     size_t workspace(int32_t tensors) const
@@ -386,6 +437,14 @@ int finish(const char *who, const double *partial, int count, double max_norm, d
     return checked_launch(who);
 }
 
+int few_norm(const char *who, const rocket_tensor *grads, int32_t tensors, double max_norm, double *norm_dev, hipStream_t stream, const ListPlan &plan)
+{
+    return plan.each<1>({grads}, tensors, [&](const auto &r, int64_t) {
+        hipLaunchKernelGGL((rt_few<false>), dim3(1), dim3(kQuarters * kThreads_), 0, stream, r, max_norm, norm_dev, 0);
+        return checked_launch(who);
+    });
+}
+
 int check_norm(const char *fn, const rocket_tensor *grads, int32_t tensors, double max_norm, const double *norm_dev, const void *ws, size_t ws_bytes)
 {
     const std::string who = std::string(fn) + ": ";
@@ -411,9 +470,11 @@ extern "C" int rocket_grad_norm(const rocket_tensor *grads, int32_t tensors, dou
 {
     const char *who = "rocket_grad_norm";
     if (const int rc = check_norm(who, grads, tensors, max_norm, norm_dev, ws, ws_bytes); rc != ROCKET_OK) return rc;
+    const ListPlan plan(grads, tensors);
+    if (plan.few()) return few_norm(who, grads, tensors, max_norm, norm_dev, static_cast<hipStream_t>(hip_stream), plan);
     double *partial = static_cast<double *>(ws);
     int count = 0;
-    if (const int rc = squares(who, grads, tensors, partial, static_cast<hipStream_t>(hip_stream), ListPlan(grads, tensors), &count); rc != ROCKET_OK) return rc;
+    if (const int rc = squares(who, grads, tensors, partial, static_cast<hipStream_t>(hip_stream), plan, &count); rc != ROCKET_OK) return rc;
     return finish(who, partial, count, max_norm, norm_dev, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -430,11 +491,16 @@ extern "C" int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor 
     if (const int rc = check_written(who, out ? out : grads, grads, nullptr, tensors); rc != ROCKET_OK) return rc;
     const ListPlan plan(grads, tensors);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (plan.few() && plan.units <= kFewScaled)
+        return plan.each<2>({grads, out ? out : grads}, tensors, [&](const auto &r, int64_t) {
+            hipLaunchKernelGGL((rt_few<true>), dim3(1), dim3(kQuarters * kThreads_), 0, stream, r, max_norm, norm_dev, out ? 0 : 1);
+            return checked_launch(who);
+        });
     double *partial = static_cast<double *>(ws);
     int count = 0;
-    int rc = squares(who, grads, tensors, partial, stream, plan, &count);
-    const bool joined = count <= kJoinedSums && plan.units > 0;
-    if (rc == ROCKET_OK && !joined) rc = finish(who, partial, count, max_norm, norm_dev, stream);
+    int rc = plan.few() ? few_norm(who, grads, tensors, max_norm, norm_dev, stream, plan) : squares(who, grads, tensors, partial, stream, plan, &count);
+    const bool joined = count > 0 && count <= kJoinedSums;
+    if (rc == ROCKET_OK && !joined && !plan.few()) rc = finish(who, partial, count, max_norm, norm_dev, stream);
     if (rc != ROCKET_OK) return rc;
     return plan.each<2>({grads, out ? out : grads}, tensors, [&](const auto &r, int64_t units) {
         by_length(plan.bytes > kKeptBytes, [&](auto once) {
