@@ -138,10 +138,11 @@ extern "C" int rocket_train_step_normed(rocket_kernels *h, const void *x_dev, in
     t.grads[2].data = f32(t.gnw);
     t.grads[3].data = f32(t.gnb);
     if (rc == ROCKET_OK) rc = rocket_grad_norm(t.grads, 4, max_norm, norm, ws, t.inner, hip_stream);
-    if (rc == ROCKET_OK) rc = rocket_sgd_update_clipped(h, f32(t.gw), f32(t.gb), lr, recentre, norm, hip_stream);
     rocket_tensor params[2] = {t.grads[2], t.grads[3]};
     params[0].data = norm_weight_dev;
     params[1].data = norm_bias_dev;
+    // first the update that may still refuse its arguments (weights that overlap)
     if (rc == ROCKET_OK) rc = rocket_sgd_tensors(params, t.grads + 2, nullptr, 2, lr, norm, hip_stream);
+    if (rc == ROCKET_OK) rc = rocket_sgd_update_clipped(h, f32(t.gw), f32(t.gb), lr, recentre, norm, hip_stream);
     return rc;
 }

@@ -168,6 +168,8 @@ def test_refusals_leave_the_parameters():
     refused(h, xd, 5, nw[:-1], nb, *args[2:], 0.1)
     refused(h, xd, 5, None, nb, *args[2:], 0.1)
     refused(h, xd, 5, *args, 0.1, workspace=torch.empty(1 << 12, dtype=torch.uint8, device="cuda"))
-    assert torch.equal(nw, m["nw"]) and torch.equal(nb, m["nb"])
+    both = torch.ones(nw.numel() + 1, device="cuda")
+    refused(h, xd, 5, both[:-1], both[1:], *args[2:], 0.1)
+    assert torch.equal(nw, m["nw"]) and torch.equal(nb, m["nb"]) and bool((both == 1.0).all())
     view = rocket.rocket_kernels_view_get(h)
     assert np.array_equal(view["weights"], kr["weights"])
