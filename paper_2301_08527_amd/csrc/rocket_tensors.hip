@@ -24,14 +24,14 @@
 
 namespace {
 
-constexpr int kThreads_ = 256;
+constexpr int kListThreads = 256;
 // Values of a unit: of the norm and the scaling 16 KB, four loads of a lane (16-bit values in units of 8 KB: 100 million in 56 us, so in 43);
 // of the update as many as there are fp32 parameters in 16 KB.
 constexpr int kUnitBytes = 16384;
 template <class T>
 constexpr int kUnit = kUnitBytes / static_cast<int>(sizeof(T));
 constexpr int kSgdUnit = kUnit<float>;
-constexpr int kMostSums = 2048;           // workgroups of all rt_squares over a list together, eight to a CU
+constexpr int kMostSums = 2048;           // workgroups of all rt_squares over a list together, eight to a CU (four: 200 million fp32 387 us, then 446)
 constexpr int kMostGroups = 1 << 20;      // of another launch (its lanes must be fewer than 2^32)
 // A list of so few units is one workgroup's: rt_few goes through 16 of them in the time of rt_squares, and no rt_finish follows (norm and
 // update of 48,000 values 18.4 us, so 14.6).  Scaling them too it beats a launch for that up to 6 (8,000 values 13.3 us, so 9.0; 64,000 would
@@ -39,7 +39,8 @@ constexpr int kMostGroups = 1 << 20;      // of another launch (its lanes must b
 constexpr int kFewUnits = 16, kFewScaled = 6;
 constexpr int kJoinedSums = 1024;         // partial sums up to which every workgroup of rt_scale adds them up itself: no rt_finish
 
-// Tensors of a launch, with POINTERS addresses each: a few, or as many as the arguments may hold.
+// Tensors of a launch, with POINTERS addresses each: a few (4 tensors with the large records 15.9 us, so 13), or as many as the
+// arguments may hold.
 constexpr int kFew = 16;
 constexpr int most_records(int pointers) { return (4096 - 128) / (8 * pointers + 4 + 2 + 1); }
 template <int POINTERS, int MOST>
@@ -67,7 +68,7 @@ __device__ __forceinline__ int tensor_of(const Records<P, M> &r, int u)
     return __builtin_amdgcn_readfirstlane(found - 1);
 }
 
-// Which units kThreads_ lanes work on, first, first + stride, ...: those of a workgroup by default.
+// Which units kListThreads lanes work on, first, first + stride, ...: those of a workgroup by default.
 struct Turn {
     int first = static_cast<int>(blockIdx.x), stride = static_cast<int>(gridDim.x), lane = static_cast<int>(threadIdx.x);
 };
@@ -96,7 +97,7 @@ __device__ __forceinline__ void each_unit(const Records<P, M> &r, const Turn &tu
     }
 }
 
-template <int THREADS = kThreads_>
+template <int THREADS = kListThreads>
 __device__ __forceinline__ double group_sum(double v, double *lds)
 {
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
@@ -123,7 +124,7 @@ __device__ __forceinline__ double squares_of(const R &r, const Turn &turn)
     double s = 0.0;
     each_unit<0>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
-        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
+        constexpr int N = kPerLoad<T>, kStep = kListThreads * N, kLoads = kUnit<T> / kStep;
         const T *g = static_cast<const T *>(r.data[0][t]) + at;
         const int i = turn.lane * N;
         typename RkSlot<T>::V v[kLoads];
@@ -140,9 +141,9 @@ __device__ __forceinline__ double squares_of(const R &r, const Turn &turn)
 }
 
 template <bool STREAM, class R>
-__global__ __launch_bounds__(kThreads_) void rt_squares(const R r, double *__restrict__ partial)
+__global__ __launch_bounds__(kListThreads) void rt_squares(const R r, double *__restrict__ partial)
 {
-    __shared__ double lds[kThreads_ / 64];
+    __shared__ double lds[kListThreads / 64];
     const double s = group_sum(squares_of<STREAM>(r, Turn()), lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
@@ -159,13 +160,13 @@ __device__ __forceinline__ double2 norm_of(const double *partial, int count, dou
 {
     double s = 0.0;
 #pragma unroll 8
-    for (int i = threadIdx.x; i < count; i += kThreads_) s += partial[i];
+    for (int i = threadIdx.x; i < count; i += kListThreads) s += partial[i];
     return norm_and_coefficient(group_sum(s, lds), max_norm);
 }
 
-__global__ __launch_bounds__(kThreads_) void rt_finish(const double *__restrict__ partial, int count, double max_norm, double *__restrict__ out)
+__global__ __launch_bounds__(kListThreads) void rt_finish(const double *__restrict__ partial, int count, double max_norm, double *__restrict__ out)
 {
-    __shared__ double lds[kThreads_ / 64];
+    __shared__ double lds[kListThreads / 64];
     const double2 n = norm_of(partial, count, max_norm, lds);
     if (threadIdx.x == 0) {
         out[0] = n.x;
@@ -179,7 +180,7 @@ __device__ __forceinline__ void scale_units(const R &r, const Turn &turn, double
 {
     each_unit<0>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
-        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kUnit<T> / kStep;
+        constexpr int N = kPerLoad<T>, kStep = kListThreads * N, kLoads = kUnit<T> / kStep;
         const T *g = static_cast<const T *>(r.data[0][t]) + at;
         T *o = static_cast<T *>(r.data[1][t]) + at;
         const int i = turn.lane * N;
@@ -198,10 +199,10 @@ __device__ __forceinline__ void scale_units(const R &r, const Turn &turn, double
 
 // count > 0: the norm is still in `count` partial sums, which every workgroup adds up; workgroup 0 writes it.
 template <bool STREAM, class R>
-__global__ __launch_bounds__(kThreads_) void rt_scale(const R r, const double *__restrict__ partial, int count, double max_norm, double *__restrict__ norm,
+__global__ __launch_bounds__(kListThreads) void rt_scale(const R r, const double *__restrict__ partial, int count, double max_norm, double *__restrict__ norm,
                                                       int in_place)
 {
-    __shared__ double lds[kThreads_ / 64];
+    __shared__ double lds[kListThreads / 64];
     double c;
     if (count > 0) {
         const double2 n = norm_of(partial, count, max_norm, lds);
@@ -217,18 +218,18 @@ __global__ __launch_bounds__(kThreads_) void rt_scale(const R r, const double *_
     scale_units<STREAM>(r, Turn(), c);
 }
 
-// A list of few units by one workgroup of kQuarters times kThreads_ lanes: the norm and, SCALE, the scaling too (every square was
+// A list of few units by one workgroup of kQuarters times kListThreads lanes: the norm and, SCALE, the scaling too (every square was
 // added before the first value is written).
 constexpr int kQuarters = 4;
 template <bool SCALE, class R>
-__global__ __launch_bounds__(kQuarters * kThreads_) void rt_few(const R r, double max_norm, double *__restrict__ norm, int in_place)
+__global__ __launch_bounds__(kQuarters * kListThreads) void rt_few(const R r, double max_norm, double *__restrict__ norm, int in_place)
 {
-    __shared__ double lds[kQuarters * kThreads_ / 64];
+    __shared__ double lds[kQuarters * kListThreads / 64];
     Turn turn;
-    turn.first = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kThreads_);
+    turn.first = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kListThreads);
     turn.stride = kQuarters;
-    turn.lane = static_cast<int>(threadIdx.x) % kThreads_;
-    const double2 n = norm_and_coefficient(group_sum<kQuarters * kThreads_>(squares_of<false>(r, turn), lds), max_norm);
+    turn.lane = static_cast<int>(threadIdx.x) % kListThreads;
+    const double2 n = norm_and_coefficient(group_sum<kQuarters * kListThreads>(squares_of<false>(r, turn), lds), max_norm);
     if (threadIdx.x == 0) {
         norm[0] = n.x;
         norm[1] = n.y;
@@ -239,13 +240,13 @@ __global__ __launch_bounds__(kQuarters * kThreads_) void rt_few(const R r, doubl
 
 // r.data: gradients, parameters, results
 template <bool STREAM, class R>
-__global__ __launch_bounds__(kThreads_) void rt_sgd(const R r, double lr, const double *__restrict__ norm)
+__global__ __launch_bounds__(kListThreads) void rt_sgd(const R r, double lr, const double *__restrict__ norm)
 {
     const double rate = norm ? lr * norm[1] : lr;
     const Turn turn;
     each_unit<kSgdUnit>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
-        constexpr int N = kPerLoad<T>, kStep = kThreads_ * N, kLoads = kSgdUnit / kStep;
+        constexpr int N = kPerLoad<T>, kStep = kListThreads * N, kLoads = kSgdUnit / kStep;
         const T *g = static_cast<const T *>(r.data[0][t]) + at;
         const float *p = static_cast<const float *>(r.data[1][t]) + at;
         float *o = static_cast<float *>(r.data[2][t]) + at;
@@ -407,8 +408,8 @@ int checked_launch(const char *who)
 
 unsigned groups_of(int64_t units) { return static_cast<unsigned>(std::min<int64_t>(units, kMostGroups)); }
 
-// What a pass leaves for the next one is kept by the caches up to here (256 MB on the memory's side); beyond, or on the way out, it
-// only displaces.
+// What a pass leaves for the next one is kept by the caches up to here (256 MB on the memory's side); beyond, it only displaces, and so do
+// results: 300 tensors (67 MB) streamed 73 us, kept 58, their results kept too 72; 200 million fp32 (800 MB) kept 414, streamed 387.
 constexpr int64_t kKeptBytes = 192 << 20;
 template <class F>
 void by_length(bool stream, F f)
@@ -424,7 +425,7 @@ int squares(const char *who, const rocket_tensor *grads, int32_t tensors, double
     return plan.each<1>({grads}, tensors, [&](const auto &r, int64_t units) {
         const int sums = static_cast<int>(plan.sums(units));
         by_length(plan.bytes > kKeptBytes, [&](auto once) {
-            hipLaunchKernelGGL((rt_squares<decltype(once)::value>), dim3(static_cast<unsigned>(sums)), dim3(kThreads_), 0, stream, r, partial + *count);
+            hipLaunchKernelGGL((rt_squares<decltype(once)::value>), dim3(static_cast<unsigned>(sums)), dim3(kListThreads), 0, stream, r, partial + *count);
         });
         *count += sums;
         return checked_launch(who);
@@ -433,14 +434,14 @@ int squares(const char *who, const rocket_tensor *grads, int32_t tensors, double
 
 int finish(const char *who, const double *partial, int count, double max_norm, double *norm_dev, hipStream_t stream)
 {
-    hipLaunchKernelGGL(rt_finish, dim3(1), dim3(kThreads_), 0, stream, partial, count, max_norm, norm_dev);
+    hipLaunchKernelGGL(rt_finish, dim3(1), dim3(kListThreads), 0, stream, partial, count, max_norm, norm_dev);
     return checked_launch(who);
 }
 
 int few_norm(const char *who, const rocket_tensor *grads, int32_t tensors, double max_norm, double *norm_dev, hipStream_t stream, const ListPlan &plan)
 {
     return plan.each<1>({grads}, tensors, [&](const auto &r, int64_t) {
-        hipLaunchKernelGGL((rt_few<false>), dim3(1), dim3(kQuarters * kThreads_), 0, stream, r, max_norm, norm_dev, 0);
+        hipLaunchKernelGGL((rt_few<false>), dim3(1), dim3(kQuarters * kListThreads), 0, stream, r, max_norm, norm_dev, 0);
         return checked_launch(who);
     });
 }
@@ -493,7 +494,7 @@ extern "C" int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor 
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (plan.few() && plan.units <= kFewScaled)
         return plan.each<2>({grads, out ? out : grads}, tensors, [&](const auto &r, int64_t) {
-            hipLaunchKernelGGL((rt_few<true>), dim3(1), dim3(kQuarters * kThreads_), 0, stream, r, max_norm, norm_dev, out ? 0 : 1);
+            hipLaunchKernelGGL((rt_few<true>), dim3(1), dim3(kQuarters * kListThreads), 0, stream, r, max_norm, norm_dev, out ? 0 : 1);
             return checked_launch(who);
         });
     double *partial = static_cast<double *>(ws);
@@ -504,7 +505,7 @@ extern "C" int rocket_grad_clip(const rocket_tensor *grads, const rocket_tensor 
     if (rc != ROCKET_OK) return rc;
     return plan.each<2>({grads, out ? out : grads}, tensors, [&](const auto &r, int64_t units) {
         by_length(plan.bytes > kKeptBytes, [&](auto once) {
-            hipLaunchKernelGGL((rt_scale<decltype(once)::value>), dim3(groups_of(units)), dim3(kThreads_), 0, stream, r, partial, joined ? count : 0, max_norm,
+            hipLaunchKernelGGL((rt_scale<decltype(once)::value>), dim3(groups_of(units)), dim3(kListThreads), 0, stream, r, partial, joined ? count : 0, max_norm,
                                norm_dev, out ? 0 : 1);
         });
         return checked_launch(who);
@@ -526,7 +527,7 @@ extern "C" int rocket_sgd_tensors(const rocket_tensor *params, const rocket_tens
     const ListPlan plan(grads, tensors, kSgdUnit);
     return plan.each<3>({grads, params, out ? out : params}, tensors, [&](const auto &r, int64_t units) {
         by_length(plan.bytes > kKeptBytes, [&](auto once) {
-            hipLaunchKernelGGL((rt_sgd<decltype(once)::value>), dim3(groups_of(units)), dim3(kThreads_), 0, static_cast<hipStream_t>(hip_stream), r, lr, norm_dev);
+            hipLaunchKernelGGL((rt_sgd<decltype(once)::value>), dim3(groups_of(units)), dim3(kListThreads), 0, static_cast<hipStream_t>(hip_stream), r, lr, norm_dev);
         });
         return checked_launch("rocket_sgd_tensors");
     });
