@@ -393,9 +393,8 @@ int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_dev, int32_
  * max_norm > 0 (INFINITY: never clips).  Squares and sums are fp64, so no finite gradient overflows or vanishes, in a fixed
  * order without atomics.  A NaN among the values makes both NaN; an infinity makes the norm infinite and the coefficient 0.
  *
- * rocket_grad_clip: rocket_grad_norm, then out[i] = grads[i] * coefficient, rounded once.  out: a list of the same counts and
- * types, or NULL: in place; where the coefficient is 1 nothing is then
- * written.
+ * rocket_grad_clip: rocket_grad_norm, then out[i] = grads[i] * coefficient in fp64, rounded to 32 bits and to its type.
+ * out: a list of the same counts and types, or NULL: in place; where the coefficient is 1 nothing is then written.
  *
  * rocket_sgd_tensors: out[i] = params[i] - lr * coefficient * grads[i], in fp64, rounded once; params and out are
  * ROCKET_F32, grads of any type, counts equal, out NULL: in place.  coefficient = norm_dev[1], or 1 where norm_dev is NULL.
