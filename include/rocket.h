@@ -384,8 +384,8 @@ int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_dev, int32_
 
 /*
  * Many tensors at once: the global norm of all gradients, clipping, and an update that clips on the way.
- * A list is a host array of `tensors` records; data is device memory (any element's address), count may be 0 (data is then
- * not looked at).  Lists are read during the call only.  Tensors that a call writes overlap neither one another nor what it reads,
+ * A list is a host array of `tensors` records; data is device memory (any element's address, of up to 48 bits), count may
+ * be 0 (data is then not looked at).  Lists are read during the call only.  Tensors that a call writes overlap neither one another nor what it reads,
  * but for the tensor that they are the new values of (ROCKET_EINVAL).  A list holds at most 2^40 values.
  *
  * rocket_grad_norm: norm = sqrt(sum of the squares of all values of all tensors), and the coefficient that brings a larger

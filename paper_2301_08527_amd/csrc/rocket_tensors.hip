@@ -39,19 +39,47 @@ constexpr int kMostGroups = 1 << 20;      // of another launch (its lanes must b
 constexpr int kFewUnits = 16, kFewScaled = 6;
 constexpr int kJoinedSums = 1024;         // partial sums up to which every workgroup of rt_scale adds them up itself: no rt_finish
 
-// Tensors of a launch, with POINTERS addresses each: a few (4 tensors with the large records 15.9 us, so 13), or as many as the
-// arguments may hold.
+// Tensors of a launch, with POINTERS addresses of 48 bits each: a few (4 tensors with the large records 15.9 us, so 13), or as many as the
+// arguments may hold: 330, 220, 165 (addresses of 64 bits, 264, 172 and 128: 300 tensors scaled 56.5 us, so 48; 150 updated 223, so 216; at 48
+// tensors of 17 MB 399 us, so 403).  The first address shares its 64 bits with what else a unit begins with, so that its loads wait for one
+// scalar load (150 tensors: 217.5 us without); the others take 32 and 16 bits, those two to a word, as no scalar load reads 16 bits (231 us).
 constexpr int kFew = 16;
-constexpr int most_records(int pointers) { return (4096 - 128) / (8 * pointers + 4 + 2 + 1); }
+constexpr int kAddressBits = 48;
+constexpr int most_records(int pointers) { return (4096 - 128) / (6 * pointers + 4 + 2); }
 template <int POINTERS, int MOST>
 struct Records {
     static constexpr int kMost = MOST;
-    void *data[POINTERS][kMost];
-    int32_t first[kMost + 1];             // unit of the launch that a tensor begins with; first[tensors]: units of the launch
-    uint16_t tail[kMost];                 // values of its last unit, less one
-    uint8_t dtype[kMost];
+    uint64_t head[MOST];                  // the first address; above it 14 bits: values of the tensor's last unit, less one; and 2: the type
+    int32_t first[MOST + 1];              // unit of the launch that a tensor begins with; first[tensors]: units of the launch
     int32_t tensors;
+    uint32_t low[POINTERS > 1 ? POINTERS - 1 : 1][POINTERS > 1 ? MOST : 1];
+    uint32_t high[POINTERS > 1 ? POINTERS - 1 : 1][POINTERS > 1 ? (MOST + 1) / 2 : 1];
+
+    // device memory, said to the compiler: for an address out of a number it takes flat loads and stores (48 tensors of 17 MB 409 us)
+    template <class T>
+    __device__ __forceinline__ T *at(int p, int t) const
+    {
+        uint64_t a = head[t] & ((uint64_t{1} << kAddressBits) - 1);
+        if (p > 0) a = static_cast<uint64_t>(high[p - 1][t >> 1] >> (t & 1) * 16 & 0xffff) << 32 | low[p - 1][t];
+        return (T *)(__attribute__((address_space(1))) T *)a;
+    }
+    __device__ __forceinline__ int type(int t) const { return static_cast<int>(head[t] >> 62); }
+    __device__ __forceinline__ int last(int t) const { return (static_cast<int>(head[t] >> kAddressBits) & 0x3fff) + 1; }
+    // t: 0, 1, ... in order
+    void set(int t, int64_t unit, const rocket_tensor &tensor, int last)
+    {
+        first[t] = static_cast<int32_t>(unit);
+        head[t] = reinterpret_cast<uintptr_t>(tensor.data) | static_cast<uint64_t>(tensor.dtype << 14 | (last - 1)) << kAddressBits;
+    }
+    void point(int p, int t, const void *data)
+    {
+        const uint64_t a = reinterpret_cast<uintptr_t>(data);
+        uint32_t &above = high[p - 1][t >> 1];
+        low[p - 1][t] = static_cast<uint32_t>(a);
+        above = t & 1 ? above | static_cast<uint32_t>(a >> 32) << 16 : static_cast<uint32_t>(a >> 32);
+    }
 };
+static_assert(kUnitBytes / 2 <= 1 << 14 && ROCKET_F16 < 4, "a tail and a type in 16 bits");
 template <int P>
 using Many = Records<P, most_records(P)>;
 static_assert(sizeof(Many<1>) <= 4000 && sizeof(Many<2>) <= 4000 && sizeof(Many<3>) <= 4000, "beside the other arguments");
@@ -87,12 +115,13 @@ __device__ __forceinline__ void each_unit(const Records<P, M> &r, const Turn &tu
         }
         const auto one = [&](auto type) {
             constexpr int kValues = UNIT > 0 ? UNIT : kUnit<decltype(type)>;
-            const int values = u + 1 == end ? static_cast<int>(r.tail[t]) + 1 : kValues;
+            const int values = u + 1 == end ? r.last(t) : kValues;
             if (values == kValues) f(type, std::true_type(), t, static_cast<int64_t>(u - begin) * kValues, kValues);
             else f(type, std::false_type(), t, static_cast<int64_t>(u - begin) * kValues, values);
         };
-        if (r.dtype[t] == ROCKET_F32) one(float());
-        else if (r.dtype[t] == ROCKET_BF16) one(rk_bf16());
+        const int type = r.type(t);
+        if (type == ROCKET_F32) one(float());
+        else if (type == ROCKET_BF16) one(rk_bf16());
         else one(rk_f16());
     }
 }
@@ -125,7 +154,7 @@ __device__ __forceinline__ double squares_of(const R &r, const Turn &turn)
     each_unit<0>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
         constexpr int N = kPerLoad<T>, kStep = kListThreads * N, kLoads = kUnit<T> / kStep;
-        const T *g = static_cast<const T *>(r.data[0][t]) + at;
+        const T *g = r.template at<const T>(0, t) + at;
         const int i = turn.lane * N;
         typename RkSlot<T>::V v[kLoads];
         load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
@@ -174,15 +203,15 @@ __global__ __launch_bounds__(kListThreads) void rt_finish(const double *__restri
     }
 }
 
-// r.data: gradients, results
+// r: gradients, results
 template <bool STREAM, class R>
 __device__ __forceinline__ void scale_units(const R &r, const Turn &turn, double c)
 {
     each_unit<0>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
         constexpr int N = kPerLoad<T>, kStep = kListThreads * N, kLoads = kUnit<T> / kStep;
-        const T *g = static_cast<const T *>(r.data[0][t]) + at;
-        T *o = static_cast<T *>(r.data[1][t]) + at;
+        const T *g = r.template at<const T>(0, t) + at;
+        T *o = r.template at<T>(1, t) + at;
         const int i = turn.lane * N;
         typename RkSlot<T>::V v[kLoads];
         load_unit<T, STREAM, kLoads>(g, i, kStep, values, whole, v);
@@ -238,7 +267,7 @@ __global__ __launch_bounds__(kQuarters * kListThreads) void rt_few(const R r, do
         if (!in_place || n.y != 1.0) scale_units<false>(r, turn, n.y);
 }
 
-// r.data: gradients, parameters, results
+// r: gradients, parameters, results
 template <bool STREAM, class R>
 __global__ __launch_bounds__(kListThreads) void rt_sgd(const R r, double lr, const double *__restrict__ norm)
 {
@@ -247,9 +276,9 @@ __global__ __launch_bounds__(kListThreads) void rt_sgd(const R r, double lr, con
     each_unit<kSgdUnit>(r, turn, [&](auto type, auto whole, int t, int64_t at, int values) {
         using T = decltype(type);
         constexpr int N = kPerLoad<T>, kStep = kListThreads * N, kLoads = kSgdUnit / kStep;
-        const T *g = static_cast<const T *>(r.data[0][t]) + at;
-        const float *p = static_cast<const float *>(r.data[1][t]) + at;
-        float *o = static_cast<float *>(r.data[2][t]) + at;
+        const T *g = r.template at<const T>(0, t) + at;
+        const float *p = r.template at<const float>(1, t) + at;
+        float *o = r.template at<float>(2, t) + at;
         const int i = turn.lane * N;
         typename RkSlot<T>::V v[kLoads];
         RkSlot<float>::V w[kLoads * N / 4];
@@ -287,6 +316,7 @@ std::string list_fault(const rocket_tensor *t, int32_t tensors, bool f32_only)
         else if (t[i].count < 0 || t[i].count > kMostValues || (values += t[i].count) > kMostValues) what = "a negative count, or more than 2^40 values";
         else if (t[i].count > 0 && !t[i].data) what = "NULL data";
         else if (t[i].count > 0 && reinterpret_cast<uintptr_t>(t[i].data) % rk_type_bytes(t[i].dtype) != 0) what = "not at an element's address";
+        else if (t[i].count > 0 && reinterpret_cast<uintptr_t>(t[i].data) >> kAddressBits != 0) what = "an address of more than 48 bits";
         if (what) return "tensor " + std::to_string(i) + ": " + what;
     }
     return "";
@@ -377,10 +407,8 @@ struct ListPlan {
             for (; i < tensors && k < R::kMost; ++i) {
                 const int64_t count = lists[0][i].count;
                 if (count == 0) continue;
-                for (int p = 0; p < P; ++p) r.data[p][k] = lists[p][i].data;
-                r.first[k] = static_cast<int32_t>(some);
-                r.tail[k] = static_cast<uint16_t>((count - 1) % values(lists[0][i]));
-                r.dtype[k++] = static_cast<uint8_t>(lists[0][i].dtype);
+                for (int p = 1; p < P; ++p) r.point(p, k, lists[p][i].data);
+                r.set(k++, some, lists[0][i], static_cast<int>((count - 1) % values(lists[0][i])) + 1);
                 some += units_of(lists[0][i]);
             }
             if (k == 0) break;

@@ -61,7 +61,7 @@ int main()
 {
     double *norm = static_cast<double *>(at(4096));
     // lists of any length, with empty tensors, one value, whole units and one more
-    for (int32_t n : {1, 2, 15, 16, 17, 127, 128, 129, 171, 172, 173, 263, 264, 265, 530, 5000}) {
+    for (int32_t n : {1, 2, 15, 16, 17, 164, 165, 166, 219, 220, 221, 329, 330, 331, 662, 5000}) {
         std::vector<rocket_tensor> g(n), o(n), p(n), q(n);
         uint64_t next = 1 << 20;
         for (int32_t i = 0; i < n; ++i) {
@@ -92,11 +92,15 @@ int main()
         }
     }
     // the largest lists: 2^40 values, and one more
-    rocket_tensor big[2] = {{at(1 << 20), (int64_t{1} << 40) - 5, ROCKET_BF16, 0}, {at(uint64_t{1} << 50), 5, ROCKET_F32, 0}};
+    rocket_tensor big[2] = {{at(1 << 20), (int64_t{1} << 40) - 5, ROCKET_BF16, 0}, {at(uint64_t{1} << 47), 5, ROCKET_F32, 0}};
     CHECK(rocket_grad_norm(big, 2, 1.0, norm, at(8192), size_t{1} << 30, nullptr) == ROCKET_OK);
     CHECK(rocket_grad_clip(big, nullptr, 2, 1.0, norm, at(8192), size_t{1} << 30, nullptr) == ROCKET_OK);
     big[1].count = 6;
     CHECK(rocket_grad_norm(big, 2, 1.0, norm, at(8192), size_t{1} << 30, nullptr) == ROCKET_EINVAL);
+    big[1] = {at(uint64_t{1} << 48), 5, ROCKET_F32, 0};
+    CHECK(rocket_grad_norm(big, 2, 1.0, norm, at(8192), size_t{1} << 30, nullptr) == ROCKET_EINVAL);
+    big[1].count = 0;
+    CHECK(rocket_grad_norm(big, 2, 1.0, norm, at(8192), size_t{1} << 30, nullptr) == ROCKET_OK);
     // the layer norm: every way a row is held, and the limits
     const void *x = at(1 << 20);
     const float *w = static_cast<const float *>(at(1 << 24));

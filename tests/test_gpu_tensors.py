@@ -133,6 +133,29 @@ def test_no_overflow_no_loss_of_small_values():
     assert rocket.rocket_grad_clip(empty, 1.0).tolist() == [0.0, 1.0]
 
 
+@pytest.mark.parametrize("tensors", [16, 17, 165, 166, 220, 221, 330, 331, 662])
+def test_lists_of_one_launch_and_one_more(tensors):
+    """Tensors of all types, with empty ones among them and several units in some, as many as a launch's records hold and one more."""
+    import torch
+    sizes = [1 + 2917 * i % 9001 + (20011 if i % 29 == 3 else 0) for i in range(tensors)]
+    for i in range(0, tensors, 11):
+        sizes.insert(i, 0)
+    grads = make(sizes, [TYPES[i % 3] for i in range(len(sizes))], tensors)
+    params = make(sizes, ["float32"] * len(sizes), tensors + 1)
+    max_norm = 0.37 * exact_norm(grads)
+    out = [torch.full_like(g, 3.0) for g in grads]
+    norm = rocket.rocket_grad_clip(grads, max_norm, out=out)
+    c = check_norm(norm, grads, max_norm)
+    new = [torch.full_like(p, 3.0) for p in params]
+    rocket.rocket_sgd_tensors(params, grads, 0.25, norm=norm, out=new)
+    for g, o, p, q in zip(grads, out, params, new):
+        check_scaled(o, g, c)
+        want = p.double() - 0.25 * c * g.double()
+        # one rounding to 32 bits, and fp64's in the product and the difference
+        tol = 2.0 ** -24 * want.abs() + 2.0 ** -51 * (p.double().abs() + g.double().abs()) + 2.0 ** -150
+        assert bool(((q.double() - want).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("where", [0, 5000, 99999])
 def test_infinities_and_nan(where):
     import torch
