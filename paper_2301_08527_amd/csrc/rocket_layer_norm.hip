@@ -185,10 +185,10 @@ __device__ __forceinline__ float rn_rstd(const Moments &m, float eps) { return 1
 // A row lies in the registers of LANES lanes, SLOTS loads of 16 bytes in each (as loaded: 16-bit values take half the registers),
 // so x is read once.  Two passes over the registers give the mean and the distances from it; up to 64 lanes meet by lane
 // exchanges alone, more lanes once through LDS, where the wavefronts' own means and sums of squares are joined.  A group of lanes has one
-// plane of ROWS examples, whose weights it loads once.  Groups of neighbouring planes lie side by side; examples from
-// `first` on.
+// plane of ROWS examples, whose weights it loads once.  Groups of neighbouring planes lie side by side; examples
+// `first` .. `end` - 1 (the last workgroup may have groups left over: what lies behind `end` is another launch's).
 template <class T, int LANES, int SLOTS, int ROWS, bool STREAM>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int first, int rows, int planes, int n,
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T *x, int first, int end, int planes, int n,
                                                                         const float *__restrict__ weight, const float *__restrict__ bias, float eps,
                                                                         T *y, float *__restrict__ mean, float *__restrict__ rstd)
 {
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T 
     const unsigned group = blockIdx.x * kGroups + threadIdx.x / LANES, block = group / static_cast<unsigned>(planes);
     const int plane = static_cast<int>(group - block * static_cast<unsigned>(planes));
     const int64_t b0 = first + static_cast<int64_t>(block) * ROWS;
-    if (LANES <= 64 && b0 >= rows) return;
+    if (LANES <= 64 && b0 >= end) return;
     const Place<T, LANES, SLOTS> place(n, lane);
     Held<T, SLOTS> raw[ROWS];
     float w[kEarly ? SLOTS : 1][N], b[kEarly ? SLOTS : 1][N];
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T 
         if (weight) rn_beside(weight + w0, place, k, ww);
         if (bias) rn_beside(bias + w0, place, k, bb);
     };
-    const auto row_of = [&](int j) { return min(b0 + j, static_cast<int64_t>(rows) - 1) * planes + plane; };       // beyond the last: the last once more
+    const auto row_of = [&](int j) { return min(b0 + j, static_cast<int64_t>(end) - 1) * planes + plane; };       // beyond the last: the last once more
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) rn_hold<T, LANES, SLOTS, STREAM>(raw[j], x + row_of(j) * n, place);
     if constexpr (kEarly)
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T 
     for (int j = 0; j < ROWS; ++j) {
         r[j] = rn_rstd(m[j], eps);
         if constexpr (sizeof(T) == 2) rn_forget<T, SLOTS>(raw[j]);
-        if (mean && lane == 0 && b0 + j < rows) {
+        if (mean && lane == 0 && b0 + j < end) {
             mean[row_of(j)] = m[j].shift + m[j].rest;
             rstd[row_of(j)] = r[j];
         }
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rn_forward(const T 
 #pragma unroll
             for (int q = 0; q < N; ++q) v[q] = static_cast<float>(raw[j][k][q]);
             rn_normal(v, m[j], r[j], w[kEarly ? k : 0], b[kEarly ? k : 0], out);
-            if (ROWS == 1 || b0 + j < rows) rn_put<T, LANES, SLOTS, STREAM>(y + row_of(j) * n, place, k, out);
+            if (ROWS == 1 || b0 + j < end) rn_put<T, LANES, SLOTS, STREAM>(y + row_of(j) * n, place, k, out);
         }
     }
 }
@@ -882,9 +882,9 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
             // examples of a launch: its groups of lanes are fewer than 2^32, and so are its lanes
             const int64_t most = kMostGroups * kGroups / planes * J;
             for (int64_t first = 0; first < rows; first += most) {
-                const int64_t groups = (std::min<int64_t>(rows - first, most) + J - 1) / J * planes;
+                const int64_t end = std::min<int64_t>(rows, first + most), groups = (end - first + J - 1) / J * planes;
                 hipLaunchKernelGGL((rn_forward<T, L, S, J, decltype(once)::value>), dim3(static_cast<unsigned>((groups + kGroups - 1) / kGroups)), dim3(L < 256 ? 256 : L), 0,
-                                   stream, x, static_cast<int>(first), rows, planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
+                                   stream, x, static_cast<int>(first), static_cast<int>(end), planes, n, weight_dev, bias_dev, eps, y, mean_dev, rstd_dev);
             }
         };
         const int64_t loads = (n + kPerLoad<T> - 1) / kPerLoad<T>;      // of 16 bytes in a row
