@@ -559,6 +559,13 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _int32(value, name):
+    """A size that the library takes in 32 bits; ctypes would drop the upper bits of a larger one and say nothing."""
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise RocketError(ROCKET_ESHAPE, "%s = %d does not fit 32 bits" % (name, value))
+    return value
+
+
 def _norm_sizes(torch, x, planes, here):
     code = _type_code(torch, x.dtype)
     if not (code is not None and x.get_device() == here and x.is_contiguous() and x.dim() == 2):
@@ -567,11 +574,13 @@ def _norm_sizes(torch, x, planes, here):
     rows, wide = x.shape
     if planes < 1 or rows < 1 or wide < 1 or wide % planes:
         raise RocketError(ROCKET_ESHAPE, "x (%d, %d) is not rows of %d planes" % (rows, wide, planes))
-    return code, rows, wide // planes
+    _int32(planes, "planes")
+    return code, _int32(rows, "rows"), _int32(wide // planes, "n")
 
 
 def rocket_layer_norm_workspace_bytes(rows, planes, n, backward=True):
-    return int(load_library().rocket_layer_norm_workspace_bytes(rows, planes, n, int(bool(backward))))
+    return int(load_library().rocket_layer_norm_workspace_bytes(_int32(rows, "rows"), _int32(planes, "planes"), _int32(n, "n"),
+                                                                int(bool(backward))))
 
 
 def rocket_layer_norm(x, weight=None, bias=None, eps=1e-5, planes=1, y=None, mean=None, rstd=None, workspace=None, stream=None):
@@ -752,7 +761,7 @@ def _normed_inputs(torch, kernels, x, feature_mask, norm_weight, norm_bias, coef
             _fits(t, (p,), torch.float32, name, here)
     _fits(coef, (p,), torch.float64, "coef", here)
     _fits(intercept, (1,), torch.float64, "intercept", here)
-    return x.shape[0], p
+    return _int32(x.shape[0], "B"), p
 
 
 def rocket_infer_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, eps=1e-5, lam=10.0, shift=-3.0,
@@ -777,11 +786,11 @@ def rocket_infer_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, 
 
 
 def rocket_infer_normed_workspace_bytes(kernels, B, feature_mask):
-    return int(load_library().rocket_infer_normed_workspace_bytes(kernels.handle, B, feature_mask))
+    return int(load_library().rocket_infer_normed_workspace_bytes(kernels.handle, _int32(B, "B"), feature_mask))
 
 
 def rocket_train_normed_workspace_bytes(kernels, B, feature_mask):
-    return int(load_library().rocket_train_normed_workspace_bytes(kernels.handle, B, feature_mask))
+    return int(load_library().rocket_train_normed_workspace_bytes(kernels.handle, _int32(B, "B"), feature_mask))
 
 
 def rocket_train_step_normed(kernels, x, feature_mask, norm_weight, norm_bias, coef, intercept, targets, lr, max_norm=float("inf"),
