@@ -355,14 +355,15 @@ int rocket_train_step(rocket_kernels *kernels, const void *x_dev, int x_is_u8, i
  * rocket_layer_norm: x_dev and y_dev (device, rows x planes x n of type dtype: ROCKET_F32, ROCKET_BF16 or ROCKET_F16; y_dev
  * may be x_dev), weight_dev and bias_dev (device, planes x n float32, either may be NULL: 1 and 0), mean_dev and rstd_dev
  * (device, rows x planes float32, both or neither NULL) receive m and r for the backward pass.  rows, planes, n >= 1,
- * planes <= 65535, n <= 2^30, eps > 0.  Squares of distances from the mean are fp32: values of a row lie within 1e18 of each other.
+ * planes <= 65535, n <= 2^30, eps > 0.  Distances from the mean are squared and summed in fp32: a row's n D^2 stays below 3e38, D being
+ * the largest |x - m| plus the mean's own rounding, 1e-5 times the largest |x| (10,000 values: D < 1.7e17).  Beyond that r is 0 or NaN.
  *
  * rocket_layer_norm_backward: from grad_y_dev (type dtype) and the forward pass's x, mean and rstd, with g = grad_y weight
  * and h = (x - m) r
  *     grad_x = r (g - mean g - h mean(g h)),   grad_weight = sum over rows of grad_y h,   grad_bias = sum of grad_y
  * grad_x_dev (type dtype) may be grad_y_dev; grad_weight_dev and grad_bias_dev (device, planes x n float32) may be NULL.
  * The rounding of mean_dev to 32 bits is made good from the row itself, so rows whose mean is large against their spread
- * lose nothing by it.  The given rstd_dev is used as it stands.
+ * lose nothing by it.  The given rstd_dev is used as it stands.  The sums of |g| and of |g (x - m)| over a row stay below 3e38 too.
  *
  * Statistics and sums are fp32 or wider and taken in a fixed order without atomics: the same call gives the same bits
  * (not the same as another number of rows would, for the sums over rows).  A row that holds a NaN or an infinity becomes NaN

@@ -1,5 +1,7 @@
 """The layer norm at sizes where its launches, its sums over rows and its ranges end (rocket_layer_norm, rocket_layer_norm_backward).
 Needs an MI355X."""
+import math
+
 import pytest
 
 from paper_2301_08527_amd import rocket
@@ -30,3 +32,46 @@ def test_in_place_over_several_launches(n, lanes):
         whole = rows // period * period
         assert bool((got[:whole].view(-1, period, got.shape[1]) == one).all())
         assert torch.equal(got[whole:], one[:rows - whole])
+
+
+@pytest.mark.parametrize("dtype,far", [("float32", False), ("float32", True), ("bfloat16", False)])
+@pytest.mark.parametrize("rows,n", [(3, 8), (3, 301), (3, 1500), (3, 10000), (259, 65001), (3, 200001)])
+def test_rows_as_large_as_their_squares_allow(rows, n, dtype, far):
+    """n D^2 just below 3e38, D the largest distance from the mean and 1e-5 times the largest value: values of +-D, or, `far`, values whose
+    mean's rounding takes nearly half of it.
+
+    Tolerances: a sum adds at most 138 numbers one after the other (128 values of a lane, 6 exchanges, 4 joins), each addition off by
+    U = 2^-24.  The first sum's rounding, `off` in units of the spread, is in the distances that the second one adds: it makes their
+    mean's error (1 + off), that of their squares (1 + off^2) times as large.  The backward pass is given that r, three times in h c2."""
+    import torch
+    U, half = 2.0 ** -24, torch.finfo(getattr(torch, dtype)).eps / 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    most = math.sqrt(2.99e38 / n)
+    w, b = 0.5 + torch.rand(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    dy = torch.randn((rows, n), generator=g, device="cuda").to(getattr(torch, dtype))
+    if far:
+        x = 0.45e5 * most + 0.27 * most * (2.0 * torch.rand((rows, n), generator=g, device="cuda") - 1.0)
+    else:
+        x = 0.99 * most * (1.0 - 2.0 * (torch.arange(n, device="cuda") % 2)).repeat(rows, 1)
+    x = x.to(getattr(torch, dtype))
+    xd = x.double()
+    m = xd.mean(1, keepdim=True)
+    d = xd - m
+    assert float(n * (d.abs().amax() + 1e-5 * xd.abs().amax()) ** 2) < 3e38
+    r = 1.0 / torch.sqrt((d * d).mean(1, keepdim=True) + 1e-5)
+    mean, rstd = torch.empty((2, rows, 1), device="cuda")
+    y = rocket.rocket_layer_norm(x, w, b, mean=mean, rstd=rstd)
+    h, off = d * r, 142 * U * float(xd.abs().amax()) * r
+    ha, wide = h.abs(), 142 * (1 + off * off)
+    want = h * w.double() + b.double()
+    assert bool(((y.double() - want).abs() <= U * (142 * (1 + off) + wide * ha) * w.double() + (2 * U + half * 1.001) * want.abs()).all())
+    assert bool(((rstd.double() - r).abs() <= U * wide * r).all())
+    dx, dw, db = rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w)
+    gd = dy.double() * w.double()
+    c1, c2 = gd.mean(1, keepdim=True), (gd * h).mean(1, keepdim=True)
+    a1, a2 = gd.abs().mean(1, keepdim=True), (gd * h).abs().mean(1, keepdim=True)
+    want = r * (gd - c1 - h * c2)
+    tol = r * U * (146 * (a1 * (1 + ha) + a2 * (2 + ha)) + 8 * gd.abs() + wide * (gd.abs() + a1 + 3 * ha * a2)) + half * 1.001 * want.abs()
+    assert bool(((dx.double() - want).abs() <= tol).all())
+    assert bool(dw.isfinite().all()) and bool(db.isfinite().all())
