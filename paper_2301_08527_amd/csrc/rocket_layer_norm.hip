@@ -602,10 +602,11 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_parts(const T *x, co
                     }
 #pragma unroll
                     for (int q = 0; q < N; ++q) {
-                        const float h = (static_cast<float>(xs[k][q]) - m) * r, g = static_cast<float>(ds[k][q]) * w[q];
+                        // (beyond the row's end x is 0 and -m r may be infinite, its product with g = 0 a NaN)
+                        const float h = whole || i + q < n ? (static_cast<float>(xs[k][q]) - m) * r : 0.f, g = static_cast<float>(ds[k][q]) * w[q];
                         s[0] += g;
                         s[1] = fmaf(g, h, s[1]);
-                        s[2] += whole || i + q < n ? h : 0.f;
+                        s[2] += h;
                     }
                 }
             });

@@ -75,3 +75,24 @@ def test_rows_as_large_as_their_squares_allow(rows, n, dtype, far):
     tol = r * U * (146 * (a1 * (1 + ha) + a2 * (2 + ha)) + 8 * gd.abs() + wide * (gd.abs() + a1 + 3 * ha * a2)) + half * 1.001 * want.abs()
     assert bool(((dx.double() - want).abs() <= tol).all())
     assert bool(dw.isfinite().all()) and bool(db.isfinite().all())
+
+
+@pytest.mark.parametrize("n", [1500, 20000, 30001])
+def test_constant_rows_whose_mean_times_rstd_overflows(n):
+    """x = m = 2^66 and r = 1 / sqrt(1e-42) = 1e21: h is 0 everywhere, also where a slot reaches beyond the row (there (0 - m) r would be
+    -inf, and its product with 0 a NaN).  What is left is r (g - mean g); its sum adds at most 80 numbers one after the other."""
+    import torch
+    U = 2.0 ** -24
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    x = torch.full((3, n), 2.0 ** 66, device="cuda")
+    w, dy = 0.5 + torch.rand(n, generator=g, device="cuda"), torch.randn((3, n), generator=g, device="cuda")
+    mean, rstd = torch.empty((2, 3, 1), device="cuda")
+    y = rocket.rocket_layer_norm(x, w, w, 1e-42, mean=mean, rstd=rstd)
+    assert torch.equal(y, w.expand(3, n)) and bool((mean == 2.0 ** 66).all())
+    dx, dw, db = rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w)
+    gd, r = dy.double() * w.double(), rstd.double()
+    want = r * (gd - gd.mean(1, keepdim=True))
+    assert bool(((dx.double() - want).abs() <= r * U * (84 * gd.abs().mean(1, keepdim=True) + 4 * gd.abs())).all())
+    assert bool((dw == 0).all())
+    assert bool(((db.double() - dy.double().sum(0)).abs() <= 4 * U * dy.double().abs().sum(0)).all())
