@@ -817,7 +817,7 @@ struct BackwardPlan {
         const int64_t tiles = (n + kNormThreads * per_load - 1) / (kNormThreads * per_load) * planes;
         const int64_t want = std::min<int64_t>(std::max<int64_t>(1, 2048 / tiles), 4096);
         per = static_cast<int>(std::max<int64_t>(8, (rows + want - 1) / want));
-        parts = (rows + per - 1) / per;
+        parts = static_cast<int>((static_cast<int64_t>(rows) + per - 1) / per);
     }
     size_t sums_bytes() const { return up256(static_cast<size_t>(R) * static_cast<size_t>(row_parts) * sizeof(float4)); }
     size_t part_bytes() const { return row_parts == 0 && parts == 1 ? 0 : up256(static_cast<size_t>(2 * parts) * static_cast<size_t>(rn_stride(wide)) * 4); }

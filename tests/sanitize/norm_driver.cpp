@@ -1,5 +1,5 @@
-// Which rows the launches of the layer norm's forward pass cover, under AddressSanitizer and UndefinedBehaviorSanitizer without a
-// GPU: a call of more rows than a launch holds is several launches, and each row belongs to one of them alone (in place, a row that
+// The layer norm's sizes up to their limits, and which rows the launches of its forward pass cover, under AddressSanitizer and
+// UndefinedBehaviorSanitizer without a GPU: a call of more rows than a launch holds is several launches, and each row belongs to one of them alone (in place, a row that
 // two launches normalise is normalised twice).  Launches are replaced by a stub that reads their arguments.
 #include <hip/hip_runtime.h>
 
@@ -96,6 +96,17 @@ static void *at(uint64_t a) { return reinterpret_cast<void *>(a); }
 
 int main()
 {
+    // workspace sizes are told for every size that the calls take, also for what no card holds; more rows never need less
+    for (int32_t n : {1, 17, 4097, 20481, 33000, 131073, 1000003, 1 << 30})
+        for (int32_t planes : {1, 3, 2048, 65535})
+            for (int backward : {0, 1}) {
+                size_t before = 0;
+                for (int32_t rows : {1, 300, 1 << 20, 1 << 30, (1 << 30) + 1, 2147483646, 2147483647}) {
+                    const size_t need = rocket_layer_norm_workspace_bytes(rows, planes, n, backward);
+                    if (need % 256 != 0 || (backward && need < 256) || (rows > 300 && need < before)) fail("bad workspace size", std::to_string(rows) + " " + std::to_string(planes) + " " + std::to_string(n));
+                    before = need;
+                }
+            }
     float *f = static_cast<float *>(at(1 << 25));
     for (int32_t type : {ROCKET_F32, ROCKET_BF16})
         for (int32_t n : {2, 16, 17, 40, 100, 200, 500, 700, 1000, 2000, 3001, 5000, 10000, 30000})

@@ -1,4 +1,4 @@
-"""Launches of the layer norm on the CPU: tests/sanitize/norm_driver.cpp, linked with the translation unit, under AddressSanitizer and
+"""Launches and sizes of the layer norm on the CPU: tests/sanitize/norm_driver.cpp, linked with the translation unit, under AddressSanitizer and
 UndefinedBehaviorSanitizer."""
 import os
 
@@ -8,7 +8,7 @@ from test_sanitizers import CSRC, ENV, HIPCC, ROCM_INCLUDE, ROOT, SAN, _run
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not found")
-def test_each_row_belongs_to_one_launch(tmp_path):
+def test_sizes_to_the_limits_and_each_row_in_one_launch(tmp_path):
     host_san = []
     for f in SAN:
         host_san += ["-Xarch_host", f]
