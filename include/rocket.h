@@ -410,7 +410,7 @@ typedef struct rocket_tensor {
     void *data;
     int64_t count;
     int32_t dtype;      /* ROCKET_F32, ROCKET_BF16, ROCKET_F16 */
-    int32_t reserved;   /* 0 */
+    int32_t reserved;   /* 0 (ROCKET_EINVAL) */
 } rocket_tensor;
 size_t rocket_grad_workspace_bytes(const rocket_tensor *grads, int32_t tensors);
 int rocket_grad_norm(const rocket_tensor *grads, int32_t tensors, double max_norm, double *norm_dev,

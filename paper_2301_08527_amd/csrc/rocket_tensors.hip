@@ -317,6 +317,7 @@ std::string list_fault(const rocket_tensor *t, int32_t tensors, bool f32_only)
         else if (t[i].count > 0 && !t[i].data) what = "NULL data";
         else if (t[i].count > 0 && reinterpret_cast<uintptr_t>(t[i].data) % rk_type_bytes(t[i].dtype) != 0) what = "not at an element's address";
         else if (t[i].count > 0 && reinterpret_cast<uintptr_t>(t[i].data) >> kAddressBits != 0) what = "an address of more than 48 bits";
+        else if (t[i].reserved != 0) what = "reserved must be 0";
         if (what) return "tensor " + std::to_string(i) + ": " + what;
     }
     return "";
