@@ -96,3 +96,20 @@ def test_constant_rows_whose_mean_times_rstd_overflows(n):
     assert bool(((dx.double() - want).abs() <= r * U * (84 * gd.abs().mean(1, keepdim=True) + 4 * gd.abs())).all())
     assert bool((dw == 0).all())
     assert bool(((db.double() - dy.double().sum(0)).abs() <= 4 * U * dy.double().abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("n", [65536 + 8192, 125000, 131072])
+def test_sums_of_many_values_of_a_lane(n):
+    """A row for each CU of so many 16-bit values that a lane holds up to 128.  Of three lanes two begin with 2^24 and one with -2^25 (but for
+    every wavefront's last lane), all other values are 1: half a step, or less, of the sum that they are added to, lost each time, so that
+    a sum of k numbers one after the other is off by k.  The mean of the distances has the error of such a sum of at most 80."""
+    import torch
+    rows, U = 256, 2.0 ** -24
+    x = torch.ones((rows, n), dtype=torch.bfloat16, device="cuda")
+    first = torch.tensor([2.0 ** 24, 2.0 ** 24, -2.0 ** 25] * 21 + [1.0], dtype=torch.bfloat16, device="cuda")
+    x[:, 0:8192:8] = first.repeat(16)
+    mean, rstd = torch.empty((2, rows, 1), device="cuda")
+    rocket.rocket_layer_norm(x, mean=mean, rstd=rstd)
+    d = x[0].double()
+    m = float(d.mean())
+    assert bool(((mean.double() - m).abs() <= U * abs(m) + 80 * U * float((d - m).abs().mean())).all())
