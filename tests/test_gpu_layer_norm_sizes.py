@@ -113,3 +113,37 @@ def test_sums_of_many_values_of_a_lane(n):
     d = x[0].double()
     m = float(d.mean())
     assert bool(((mean.double() - m).abs() <= U * abs(m) + 80 * U * float((d - m).abs().mean())).all())
+
+
+SUMS = [(8191, 1, 7), (70001, 1, 3), (70001, 2, 30), (40009, 1, 65), (5003, 1025, 5), (9001, 3, 129), (20011, 1, 250), (20011, 1, 501), (8209, 1, 1000),
+        (20011, 2, 1537), (4001, 1, 2050), (1201, 257, 2049), (401, 257, 4099), (677, 2, 10000), (3001, 1, 16384), (2003, 1, 20480), (5, 1, 20481), (3001, 1, 30001),
+        (400009, 1, 2048)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,planes,n", SUMS)
+def test_sums_over_rows_miss_no_row_and_take_none_twice(rows, planes, n, dtype):
+    """Gradients of -3 .. 3 and values of -1, 0 and 1 with a mean of 0, given an rstd of 1/2: every term of both sums is a multiple of 1/2 and
+    every sum below 2^22, so that they are exact in whatever order and every single row counts."""
+    import torch
+    print("sums over rows", rows, planes, n, dtype, flush=True)
+    t = getattr(torch, dtype)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + n)
+    x = torch.zeros((rows, planes, n), dtype=t, device="cuda")
+    half = n // 2
+    dy = torch.empty_like(x)
+    dw, db = torch.zeros((2, planes, n), dtype=torch.float64, device="cuda")
+    step = max(1, (1 << 26) // (planes * n))
+    for i in range(0, rows, step):
+        some = min(step, rows - i)
+        sign = (2 * torch.randint(0, 2, (some, planes, half), generator=g, device="cuda") - 1).to(t)
+        x[i:i + some, :, :half], x[i:i + some, :, n - half:] = sign, -sign
+        dy[i:i + some] = torch.randint(-3, 4, (some, planes, n), generator=g, device="cuda").to(t)
+        d = dy[i:i + some].double()
+        dw += (d * x[i:i + some].double()).sum(0) / 2
+        db += d.sum(0)
+    mean, rstd = torch.zeros((rows, planes), device="cuda"), torch.full((rows, planes), 0.5, device="cuda")
+    w = torch.rand(planes * n, generator=g, device="cuda")
+    _, gw, gb = rocket.rocket_layer_norm_backward(x.view(rows, -1), dy.view(rows, -1), mean, rstd, w, planes)
+    assert torch.equal(gw.double().view(planes, n), dw) and torch.equal(gb.double().view(planes, n), db)
