@@ -369,7 +369,8 @@ int rocket_train_step(rocket_kernels *kernels, const void *x_dev, int x_is_u8, i
  * (not the same as another number of rows would, for the sums over rows).  A row that holds a NaN or an infinity becomes NaN
  * as the formulas have it and leaves the other rows as they are (grad_weight and grad_bias sum over it).
  * workspace_dev: rocket_layer_norm_workspace_bytes(rows, planes, n, backward) bytes of device memory, 256-byte aligned;
- * the forward pass needs none (0 bytes, NULL allowed) unless rows are longer than a workgroup holds.  0 on invalid sizes.
+ * the forward pass needs none (0 bytes, NULL allowed) unless rows are longer than a workgroup holds.  They hold for every call of
+ * as many rows or fewer.  0 on invalid sizes.
  * Every pointer is of the device that is current and of elements of its type (any element's address will do).
  * Asynchronous on hip_stream, allocates nothing, may be captured.
  */

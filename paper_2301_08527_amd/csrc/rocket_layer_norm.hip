@@ -779,6 +779,7 @@ constexpr double kHeldKeptBytes = 128 << 20;
 struct BackwardPlan {
     int64_t R, wide;
     int lanes = 0, slots = 0, parts = 1;
+    int most_parts = 1;                           // of as many rows or fewer
     int row_parts = 0, length = 0, per = 0;       // two passes: parts of a row, their length; rows of a part
     bool once = false;                            // nothing is kept by the caches; of two passes: for the second
     BackwardPlan(int32_t rows, int32_t planes, int32_t n, int32_t dtype) : R(static_cast<int64_t>(rows) * planes), wide(static_cast<int64_t>(planes) * n)
@@ -806,7 +807,7 @@ struct BackwardPlan {
             const int64_t most = std::max<int64_t>(1, (lanes <= 64 ? 256 / slots : 256) * 1024 / threads / planes);
             // a few turns of one workgroup take less than the second launch (2 x 500 fp32, 32 examples: 10.3 us, with it 12.3; 64: 17.4 and 12.2;
             // 2 x 10,000, 4 examples: 11 and 13.5, 16: 45 and 13)
-            parts = static_cast<int>(std::min(most, turns <= (lanes <= 64 || slots == 1 ? 8 : 4) ? 1 : turns));
+            parts = most_parts = static_cast<int>(std::min(most, turns <= (lanes <= 64 || slots == 1 ? 8 : 4) ? 1 : turns));
             if (parts > 1) parts = static_cast<int>((turns + (turns + parts - 1) / parts - 1) / ((turns + parts - 1) / parts));     // all take as many turns
             return;
         }
@@ -818,10 +819,12 @@ struct BackwardPlan {
         const int64_t want = std::min<int64_t>(std::max<int64_t>(1, 2048 / tiles), 4096);
         per = static_cast<int>(std::max<int64_t>(8, (rows + want - 1) / want));
         parts = static_cast<int>((static_cast<int64_t>(rows) + per - 1) / per);
+        most_parts = static_cast<int>(std::min(want, (static_cast<int64_t>(rows) + 7) / 8));
     }
     size_t sums_bytes() const { return up256(static_cast<size_t>(R) * static_cast<size_t>(row_parts) * sizeof(float4)); }
-    size_t part_bytes() const { return row_parts == 0 && parts == 1 ? 0 : up256(static_cast<size_t>(2 * parts) * static_cast<size_t>(rn_stride(wide)) * 4); }
-    size_t bytes() const { return std::max<size_t>(256, sums_bytes() + part_bytes()); }
+    size_t part_bytes(int count) const { return row_parts == 0 && count == 1 ? 0 : up256(static_cast<size_t>(2 * count) * static_cast<size_t>(rn_stride(wide)) * 4); }
+    size_t bytes() const { return std::max<size_t>(256, sums_bytes() + part_bytes(parts)); }
+    size_t most_bytes() const { return std::max<size_t>(256, sums_bytes() + part_bytes(most_parts)); }
 };
 
 // f(Int<v>) where v is one of FROM .. TO
@@ -854,9 +857,10 @@ bool misaligned(const void *p, int32_t dtype) { return reinterpret_cast<uintptr_
 extern "C" size_t rocket_layer_norm_workspace_bytes(int32_t rows, int32_t planes, int32_t n, int backward)
 {
     if (rows < 1 || planes < 1 || n < 1 || planes > kMostPlanes || n > kMostValues) return 0;
-    // the call's element type is not known here: fp32 rows take the most parts
-    return backward ? std::max(BackwardPlan(rows, planes, n, ROCKET_F32).bytes(), BackwardPlan(rows, planes, n, ROCKET_BF16).bytes())
-                    : ForwardPlan(rows, planes, n, ROCKET_F32).bytes();
+    // the call's element type is not known here (fp32 rows take the most parts), and its rows may be fewer: the last batch of many
+    if (backward) return std::max(BackwardPlan(rows, planes, n, ROCKET_F32).most_bytes(), BackwardPlan(rows, planes, n, ROCKET_BF16).most_bytes());
+    const int32_t few = std::min(rows, (kCus - 1) / planes);      // that leave CUs without a row may go in parts where more do not
+    return std::max(ForwardPlan(rows, planes, n, ROCKET_F32).bytes(), few > 0 ? ForwardPlan(few, planes, n, ROCKET_F32).bytes() : 0);
 }
 
 extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows, int32_t planes, int32_t n, const float *weight_dev,
@@ -937,7 +941,7 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
         return rk_fail(ROCKET_EWORKSPACE, "rocket_layer_norm_backward: an aligned workspace of " + std::to_string(plan.bytes()) + " bytes required");
     const bool sums_wanted = grad_weight_dev || grad_bias_dev;
     float4 *sums = static_cast<float4 *>(ws);
-    float *part = sums_wanted && plan.part_bytes() > 0 ? reinterpret_cast<float *>(static_cast<char *>(ws) + plan.sums_bytes()) : nullptr;
+    float *part = sums_wanted && plan.part_bytes(plan.parts) > 0 ? reinterpret_cast<float *>(static_cast<char *>(ws) + plan.sums_bytes()) : nullptr;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     by_type(dtype, [&](auto t) {
         using T = decltype(t);

@@ -147,3 +147,21 @@ def test_sums_over_rows_miss_no_row_and_take_none_twice(rows, planes, n, dtype):
     w = torch.rand(planes * n, generator=g, device="cuda")
     _, gw, gb = rocket.rocket_layer_norm_backward(x.view(rows, -1), dy.view(rows, -1), mean, rstd, w, planes)
     assert torch.equal(gw.double().view(planes, n), dw) and torch.equal(gb.double().view(planes, n), db)
+
+
+@pytest.mark.parametrize("rows,less,planes,n", [(677, 640, 2, 10000), (2100, 2048, 2, 500), (1500, 1080, 1, 30000), (300, 100, 1, 40000)])
+def test_one_workspace_for_an_epoch(rows, less, planes, n):
+    """the last batch, which is smaller, in the workspaces of the others, nothing beyond them is written"""
+    import torch
+    ws, wf = (torch.full((rocket.rocket_layer_norm_workspace_bytes(rows, planes, n, b) + 256,), 7, dtype=torch.uint8, device="cuda") for b in (True, False))
+    for r in (rows, less):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(r)
+        x, dy = torch.randn((2, r, planes * n), generator=g, device="cuda")
+        w = torch.rand(planes * n, generator=g, device="cuda")
+        mean, rstd = torch.empty((2, r, planes), device="cuda")
+        y = rocket.rocket_layer_norm(x, w, planes=planes, mean=mean, rstd=rstd, workspace=wf[:-256])
+        assert torch.equal(y, rocket.rocket_layer_norm(x, w, planes=planes))
+        got = rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, planes, workspace=ws[:-256])
+        assert all(torch.equal(a, b) for a, b in zip(got, rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, planes)))
+    assert bool((ws[-256:] == 7).all()) and bool((wf[-256:] == 7).all())
