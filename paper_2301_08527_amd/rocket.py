@@ -610,8 +610,9 @@ def rocket_layer_norm(x, weight=None, bias=None, eps=1e-5, planes=1, y=None, mea
 
 
 def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, grad_x=None, grad_weight=None, grad_bias=None,
-                               workspace=None, stream=None):
-    """Returns (grad_x of x's type, grad_weight, grad_bias float32 (planes * n,)).  grad_x may be grad_y."""
+                               workspace=None, stream=None, param_grads=True):
+    """Returns (grad_x of x's type, grad_weight, grad_bias float32 (planes * n,)).  grad_x may be grad_y.  param_grads=False
+    leaves out what grad_weight and grad_bias are not given for (None is returned for it): a norm that is not trained."""
     import torch
     here = _here(torch)
     code, rows, n = _norm_sizes(torch, x, planes, here)
@@ -629,15 +630,15 @@ def rocket_layer_norm_backward(x, grad_y, mean, rstd, weight=None, planes=1, gra
     queue = _queue(torch, stream, here)
     if grad_x is None:
         grad_x = _empty(torch, x.shape, x.dtype, stream)
-    if grad_weight is None:
+    if grad_weight is None and param_grads:
         grad_weight = _empty(torch, (planes * n,), torch.float32, stream)
-    if grad_bias is None:
+    if grad_bias is None and param_grads:
         grad_bias = _empty(torch, (planes * n,), torch.float32, stream)
     need = 0 if workspace is not None else rocket_layer_norm_workspace_bytes(rows, planes, n, True)
     ws, size, keep = _scratch(torch, need, workspace, stream, here)
     _check(load_library().rocket_layer_norm_backward(
         x.data_ptr(), grad_y.data_ptr(), code, rows, planes, n, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), grad_x.data_ptr(),
-        grad_weight.data_ptr(), grad_bias.data_ptr(), ws, size, queue))
+        _ptr(grad_weight), _ptr(grad_bias), ws, size, queue))
     return grad_x, grad_weight, grad_bias
 
 

@@ -165,3 +165,21 @@ def test_one_workspace_for_an_epoch(rows, less, planes, n):
         got = rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, planes, workspace=ws[:-256])
         assert all(torch.equal(a, b) for a, b in zip(got, rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, planes)))
     assert bool((ws[-256:] == 7).all()) and bool((wf[-256:] == 7).all())
+
+
+@pytest.mark.parametrize("rows,planes,n", [(7, 2, 300), (64, 1, 9000), (700, 2, 1537), (9, 1, 40000)])
+def test_a_norm_that_is_not_trained(rows, planes, n):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    x, dy = torch.randn((2, rows, planes * n), generator=g, device="cuda")
+    w = torch.rand(planes * n, generator=g, device="cuda")
+    mean, rstd = torch.empty((2, rows, planes), device="cuda")
+    rocket.rocket_layer_norm(x, w, planes=planes, mean=mean, rstd=rstd)
+    back = lambda **k: rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, planes, **k)
+    dx, dw, db = back()
+    got = back(param_grads=False)
+    assert torch.equal(got[0], dx) and got[1] is None and got[2] is None
+    mine = torch.empty_like(db)
+    got = back(param_grads=False, grad_bias=mine)       # one of the two
+    assert torch.equal(got[0], dx) and got[1] is None and got[2] is mine and torch.equal(mine, db)
