@@ -71,24 +71,24 @@ __device__ __forceinline__ typename RkSlot<T>::V rk_load_edge(const T *p, int i,
 }
 
 // N fp32 values from p on
-template <int N, bool STREAM = false>
+template <int N>
 __device__ __forceinline__ void rk_load_f32(const float *p, float (&v)[N])
 {
 #pragma unroll
     for (int k = 0; k < N; k += 4) {
-        const RkSlot<float>::V q = rk_load_slot<float, STREAM>(p + k);
+        const RkSlot<float>::V q = rk_load_slot<float, false>(p + k);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[k + j] = q[j];
     }
 }
 
-// values i .. i + N - 1 of a run of n that starts at p, zeros beyond its end
-template <int N, bool TINY>
+// values i .. i + N - 1 of a run of n, four at least, that starts at p, zeros beyond its end
+template <int N>
 __device__ __forceinline__ void rk_load_f32_edge(const float *p, int i, int n, float (&v)[N])
 {
 #pragma unroll
     for (int k = 0; k < N; k += 4) {
-        const RkSlot<float>::V q = rk_load_edge<float, false, TINY>(p, i + k, n);
+        const RkSlot<float>::V q = rk_load_edge<float, false, false>(p, i + k, n);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[k + j] = q[j];
     }

@@ -346,7 +346,7 @@ __device__ __forceinline__ Moments rn_row_moments(const float4 *moments, int par
 // What is written is never kept for the next kernel at the cost of what the caches hold, what is read for the last time (ONCE) neither where
 // they did not keep it anyway: 1,000 x 50,000 fp32 128 us, so 108; 1,000 x 150,000 347, so 313.
 template <class T, bool ONCE>
-__global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int64_t R, int planes, int n, int length, int parts,
+__global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int64_t R, int planes, int n, int parts,
                                                                  const float4 *__restrict__ moments, const float *__restrict__ weight,
                                                                  const float *__restrict__ bias, float eps, T *y, float *__restrict__ mean,
                                                                  float *__restrict__ rstd)
@@ -368,11 +368,11 @@ __global__ __launch_bounds__(kNormThreads) void rn_forward_apply(const T *x, int
                 for (int q = 0; q < N; ++q) v[q] = static_cast<float>(raw[k][q]), w[q] = 1.f, b[q] = 0.f;
                 if (weight) {
                     if constexpr (whole) rk_load_f32<N>(weight + w0 + i, w);
-                    else rk_load_f32_edge<N, false>(weight + w0, i, n, w);
+                    else rk_load_f32_edge<N>(weight + w0, i, n, w);
                 }
                 if (bias) {
                     if constexpr (whole) rk_load_f32<N>(bias + w0 + i, b);
-                    else rk_load_f32_edge<N, false>(bias + w0, i, n, b);
+                    else rk_load_f32_edge<N>(bias + w0, i, n, b);
                 }
                 rn_normal(v, m, r, w, b, out);
                 if (whole || i < n) rk_store<T, true>(y + row * n + i, whole ? N : n - i, out);
@@ -598,7 +598,7 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_parts(const T *x, co
                     for (int q = 0; q < N; ++q) w[q] = 1.f;
                     if (weight) {
                         if constexpr (whole) rk_load_f32<N>(weight + w0 + i, w);
-                        else rk_load_f32_edge<N, false>(weight + w0, i, n, w);
+                        else rk_load_f32_edge<N>(weight + w0, i, n, w);
                     }
 #pragma unroll
                     for (int q = 0; q < N; ++q) {
@@ -646,7 +646,7 @@ __global__ __launch_bounds__(kNormThreads) void rn_backward_columns(const T *x, 
     float w[N], dw[N] = {}, db[N] = {}, v[N];
 #pragma unroll
     for (int q = 0; q < N; ++q) w[q] = 1.f;
-    if (weight) rk_load_f32_edge<N, false>(weight + static_cast<int64_t>(plane) * n, i, n, w);
+    if (weight) rk_load_f32_edge<N>(weight + static_cast<int64_t>(plane) * n, i, n, w);
     const int from = z * per, to = static_cast<int>(min(static_cast<int64_t>(rows), static_cast<int64_t>(from) + per));
     for (int at = from; at < to; at += kRowsAtOnce) {
         const int some = min(to - at, kRowsAtOnce);
@@ -771,7 +771,8 @@ struct ForwardPlan {
 };
 
 // One pass of the backward pass streams x, dy and dx where they are more than this: 677 x 2 x 10,000 fp32 (162 MB) 43 us, so 40.5, 65,536 x 2,048
-// bf16 159 and 149, but 400 x 10,000 fp32 (48 MB) 19.6, and would be 22, 5,000 x 1,000 18.3 and 20.5.
+// bf16 159 and 149, but 400 x 10,000 fp32 (48 MB) 19.6, and would be 22, 5,000 x 1,000 18.3 and 20.5.  Rows of four lanes are never streamed: several
+// share a cache line, and where planes lie between them that costs (3,000,000 x 2 x 13 fp32 309 us, streamed 439; 3,000,000 x 16 114 and 106).
 constexpr double kHeldKeptBytes = 128 << 20;
 
 // The backward pass.  `lanes` x `slots` hold a row (0: rows are too long and go in two passes); the rows of a plane are dealt out
@@ -897,7 +898,8 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
             // lanes to a row, slots, rows at a time: with one slot fewer, or fewer lanes, the row would not fit
             const int s64 = static_cast<int>((loads + 63) / 64), s256 = static_cast<int>((loads + 255) / 256), s1024 = static_cast<int>((loads + 1023) / 1024);
             const auto held = [&](auto lanes, auto slots, auto rows_at_once) {
-                by_kept(plan.once, [&](auto once) { launch(lanes, slots, rows_at_once, once); });
+                if constexpr (decltype(lanes)::value > 4) by_kept(plan.once, [&](auto once) { launch(lanes, slots, rows_at_once, once); });
+                else launch(lanes, slots, rows_at_once, std::false_type());       // such rows are no whole lines
             };
             const auto pick = [&](auto lanes, auto slots) {
                 plan.R >= kTwoRows ? held(lanes, slots, Int<2>()) : launch(lanes, slots, Int<1>(), std::false_type());
@@ -918,7 +920,7 @@ extern "C" int rocket_layer_norm(const void *x_dev, int32_t dtype, int32_t rows,
                                moments);
             by_kept(plan.once, [&](auto once) {
                 hipLaunchKernelGGL((rn_forward_apply<T, decltype(once)::value>), dim3(static_cast<unsigned>((n + int64_t{kPart<T>} - 1) / kPart<T>), tall),
-                                   dim3(kNormThreads), 0, stream, x, plan.R, planes, n, plan.length, plan.parts, moments, weight_dev, bias_dev, eps, y,
+                                   dim3(kNormThreads), 0, stream, x, plan.R, planes, n, plan.parts, moments, weight_dev, bias_dev, eps, y,
                                    mean_dev, rstd_dev);
             });
         }
@@ -950,10 +952,12 @@ extern "C" int rocket_layer_norm_backward(const void *x_dev, const void *grad_y_
         const auto held = [&](auto lanes, auto slots) {
             constexpr int L = decltype(lanes)::value, S = decltype(slots)::value, G = L < 256 ? 256 / L : 1;
             if (plan.lanes != L || plan.slots != S) return;
-            by_kept(plan.once && L > 4, [&](auto once) {
+            const auto run = [&](auto once) {
                 hipLaunchKernelGGL((rn_backward<T, L, S, G, decltype(once)::value>), dim3(static_cast<unsigned>(plan.parts), static_cast<unsigned>(planes)),
                                    dim3(L * G), 0, stream, x, dy, rows, planes, n, weight_dev, mean_dev, rstd_dev, dx, part, grad_weight_dev, grad_bias_dev);
-            });
+            };
+            if constexpr (L > 4) by_kept(plan.once, run);
+            else run(std::false_type());
         };
         held(Int<4>(), Int<1>());
         held(Int<8>(), Int<1>());
