@@ -745,10 +745,13 @@ using Int = std::integral_constant<int, V>;
 
 // x and y are streamed, not kept by the caches, where they are more than those hold and their rows are whole cache lines but
 // for a few: 65,536 x 2,048 bf16 102 us, so 97; 1,000,000 x 64 bf16 49, so 46; but 256 x 3 x 10,000 fp32 (62 MB) 13.3, and would be 15.7;
-// 2,000,000 x 3 x 16 fp32 138, and 147.
+// 2,000,000 x 3 x 16 fp32 138, and 147.  Fewer than kTwoRows rows of 65 loads to 4,096 are kept whatever their bytes (2,000 x 16,384 fp32 51.4 us,
+// streamed 50.6; 1,900 x 32,768 bf16 50.5 and 48.8).
 constexpr double kKeptBytes = 192 << 20;
-// From so many rows on a group of lanes takes two of a plane, whose weights it then loads once: 60,001 x 3 x 1,537 bf16 297 us, so 240;
-// 16,384 x 2 x 10,000 fp32 508, so 482.  Fewer rows are spread over the chip.
+// From so many rows on, those of all planes counted, a group of lanes takes two examples of a plane, whose weights it then loads once:
+// 60,001 x 3 x 1,537 bf16 297 us, so 240; 16,384 x 2 x 10,000 fp32 508, so 482.  Fewer rows are taken one by one (700 x 3 x 1,000 fp32, 2,100 rows of 700
+// examples: 5.4 us, one by one 4.5).  Rows of up to 64 loads are taken four examples at a time however few they are (1,000 x 256 fp32
+// 3.2 us, one by one 2.3).
 constexpr int64_t kTwoRows = 2048;
 // How a row is held: in registers as long as kMostSlots loads of 1,024 lanes hold it, else in parts.  Of more than kFewSlots only if there
 // is a row for each CU: 500 x 125,000 bf16 74.5 us in parts, 57 so; 1,000 x 65,000 fp32 142 and 114; but 64 x 100,000 f16 16 and 19.6.

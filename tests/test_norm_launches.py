@@ -14,12 +14,12 @@ def test_sizes_to_the_limits_and_each_row_in_one_launch(tmp_path):
         host_san += ["-Xarch_host", f]
     common = ["-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     objs = []
-    # the kernels are compiled for the GPU without optimisation of their own: only the host's side runs
-    for src, extra in ((os.path.join(CSRC, "rocket_layer_norm.hip"), ["--offload-arch=gfx950", "-Xarch_device", "-O1"]),
+    # only the host's side is compiled; the image with the kernels, whose address the driver's registration never looks at, is not there
+    for src, extra in ((os.path.join(CSRC, "rocket_layer_norm.hip"), ["--offload-arch=gfx950", "--offload-host-only"]),
                        (os.path.join(ROOT, "tests", "sanitize", "norm_driver.cpp"), ["-x", "c++", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INCLUDE])):
         obj = str(tmp_path / (os.path.basename(src) + ".o"))
         _run([HIPCC] + extra + common + host_san + ["-c", src, "-o", obj])
         objs.append(obj)
     exe = str(tmp_path / "norm_driver")
-    _run([HIPCC, "--offload-arch=gfx950"] + host_san + objs + ["-o", exe])
+    _run([HIPCC, "--offload-arch=gfx950"] + host_san + ["-Wl,--unresolved-symbols=ignore-in-object-files"] + objs + ["-o", exe])
     assert "norm driver: ok" in _run([exe], env=ENV)
