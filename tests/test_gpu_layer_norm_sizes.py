@@ -117,7 +117,7 @@ def test_sums_of_many_values_of_a_lane(n):
 
 SUMS = [(8191, 1, 7), (70001, 1, 3), (70001, 2, 30), (40009, 1, 65), (5003, 1025, 5), (9001, 3, 129), (20011, 1, 250), (20011, 1, 501), (8209, 1, 1000),
         (20011, 2, 1537), (4001, 1, 2050), (1201, 257, 2049), (401, 257, 4099), (677, 2, 10000), (3001, 1, 16384), (2003, 1, 20480), (5, 1, 20481), (3001, 1, 30001),
-        (400009, 1, 2048)]
+        (33001, 1, 20485), (7, 65535, 3), (400009, 1, 2048)]
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
@@ -183,3 +183,76 @@ def test_a_norm_that_is_not_trained(rows, planes, n):
     mine = torch.empty_like(db)
     got = back(param_grads=False, grad_bias=mine)       # one of the two
     assert torch.equal(got[0], dx) and got[1] is None and got[2] is mine and torch.equal(mine, db)
+
+
+def test_more_long_rows_than_a_launch_has_groups_for():
+    """33,001 rows in parts, in place; row 1,000 i + k is row k"""
+    import torch
+    rows, n, period = 33001, 65537, 1000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    small = 3.0 + torch.randn((period, n), generator=g, device="cuda")
+    w, b = torch.rand(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    mean, rstd = torch.empty((2, period, 1), device="cuda")
+    want = rocket.rocket_layer_norm(small, w, b, mean=mean, rstd=rstd)
+    x = small.repeat(rows // period + 1, 1)[:rows]
+    ms, rs = torch.empty((2, rows, 1), device="cuda")
+    rocket.rocket_layer_norm(x, w, b, y=x, mean=ms, rstd=rs)
+    for got, one in ((x, want), (ms, mean), (rs, rstd)):
+        assert all(torch.equal(got[i:i + period], one[:rows - i]) for i in range(0, rows, period))
+
+
+@pytest.mark.parametrize("rows,planes,n", [(5, 2, 3), (9, 3, 130), (6, 1, 1537), (3, 2, 9001), (2, 1, 70001)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_every_tensor_begins_anywhere(rows, planes, n, dtype):
+    """one element behind a boundary, weights, results and sums too, the same bits as elsewhere; what lies around them stays"""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    t = getattr(torch, dtype)
+    x, dy = (torch.randn((rows, planes * n), generator=g, device="cuda").to(t) for _ in range(2))
+    w, b = (torch.randn(planes * n, generator=g, device="cuda") for _ in range(2))
+    mean, rstd = torch.empty((2, rows, planes), device="cuda")
+    want = [rocket.rocket_layer_norm(x, w, b, planes=planes, mean=mean, rstd=rstd), mean, rstd]
+    want += rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, planes)
+    around = []
+
+    def moved(like, fill=True):
+        around.append(torch.full((like.numel() + 2,), 3.0, dtype=like.dtype, device="cuda"))
+        inside = around[-1][1:-1].view(like.shape)
+        return inside.copy_(like) if fill else inside
+
+    x, dy, w, b = (moved(v) for v in (x, dy, w, b))
+    y, m, r, dx, dw, db = got = [moved(v, False) for v in want]
+    rocket.rocket_layer_norm(x, w, b, planes=planes, y=y, mean=m, rstd=r)
+    rocket.rocket_layer_norm_backward(x, dy, m, r, w, planes, grad_x=dx, grad_weight=dw, grad_bias=db)
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+    assert all(bool((v[0] == 3.0) & (v[-1] == 3.0)) for v in around)
+
+
+def test_the_longest_row():
+    """2^30 - 3 values in 64 parts of 2,048 pieces, each joined with the ones before: a sum adds at most 48 + 5 * 2,048 + 40 < 10,400 numbers one
+    after the other; mean and spread of the distances have such sums' errors, and there are a few roundings of h w + b"""
+    import torch
+    n, U, half = 2 ** 30 - 3, 2.0 ** -24, 2.0 ** -8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x = (5.0 + torch.randn(n, generator=g, device="cuda")).to(torch.bfloat16).view(1, n)
+    w = torch.rand(n, generator=g, device="cuda")
+    mean, rstd = torch.empty((2, 1, 1), device="cuda")
+    y = rocket.rocket_layer_norm(x, w, mean=mean, rstd=rstd)
+    step = 1 << 27
+    m = sum(float(x[0, i:i + step].double().sum()) for i in range(0, n, step)) / n
+    r = 1.0 / math.sqrt(sum(float((x[0, i:i + step].double() - m).square().sum()) for i in range(0, n, step)) / n + 1e-5)
+    assert abs(float(mean) - m) <= U * m + 10400 * U / r and abs(float(rstd) - r) <= 10400 * U * r
+    for i in range(0, n, step):
+        h, ww = (x[0, i:i + step].double() - m) * r, w[i:i + step].double()
+        assert bool(((y[0, i:i + step].double() - h * ww).abs() <= U * 10404 * ww * (1 + h.abs()) + (U + half * 1.001) * (h * ww).abs()).all())
+    # the sums over a single row are dy h and dy themselves, but for the mean's rounding
+    dy = torch.randint(-3, 4, (1, n), generator=g, device="cuda").to(torch.bfloat16)
+    _, dw, db = rocket.rocket_layer_norm_backward(x, dy, mean, rstd, w, grad_x=y)
+    rstd = float(rstd)
+    for i in range(0, n, step):
+        d, h = dy[0, i:i + step].double(), (x[0, i:i + step].double() - m) * rstd
+        assert torch.equal(db[i:i + step].double(), d)
+        assert bool(((dw[i:i + step].double() - d * h).abs() <= U * d.abs() * (8 * h.abs() + 10400)).all())
